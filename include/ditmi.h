@@ -254,6 +254,149 @@ dit_status dit_serve(const dit_shape *s, const dit_step_weights *w, const dit_co
  * hidden must be a multiple of 4. */
 dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, float *pos, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Stand-alone operators.  The conventions above hold: device pointers, the
+ * caller's workspace and stream, everything checked before the first launch,
+ * no allocation, no atomics, results that do not depend on earlier calls.
+ * What the host cannot see (the int32 index arrays on the device) is bounded
+ * by the kernels: an entry out of range is clamped into it, so such a call
+ * computes something useless but stays inside the tensors.  Outputs must not
+ * overlap inputs unless said otherwise.
+ * ------------------------------------------------------------------------ */
+
+/* Masked attention over documents (requests, samples): packed one behind the
+ * other in one sequence, padded to equal rooms, or single new tokens over the
+ * rooms of a cache.  The block's own attention knows one length per batch and
+ * no mask; this is the attention of a batch of mixed resolutions, of padded
+ * text, of prefix-conditioned generation.
+ *
+ * Document d has query rows q_start[d] .. q_start[d+1]-1 (nq of them) of q
+ * and o, and key rows k_start[d] .. k_start[d]+nk-1 of k and v, with
+ * nk = min(k_len[d], k_start[d+1] - k_start[d]).  For its query i, key j and
+ * head h (keys of head h / (heads / kv_heads)):
+ *   s = scale * q.k
+ *   s = cap * tanh(s / cap)                     where cap > 0
+ *   s = s - slopes[h] * |i + nk - nq - j|       where slopes is given
+ *   j is visible when j < nk and
+ *     DIT_MASK_FULL    always
+ *     DIT_MASK_CAUSAL  j <= i + nk - nq         (the last query sees every key)
+ *     DIT_MASK_PREFIX  j <= i + nk - nq or j < prefix[d]
+ *   o = softmax over the visible keys of s, times v
+ * A query without a visible key gets zeros.  What k and v hold in rows that a
+ * query cannot see (NaN and infinities included) does not reach it.  A score
+ * of -inf counts as not visible.  Rows of o outside every document are left
+ * as they were.  fp32 softmax and sums; in bf16 the probabilities, taken
+ * relative to a running maximum, are rounded to bf16 before the product with
+ * v, and their sum is that of the rounded ones.
+ *   docs >= 1;  heads a multiple of kv_heads;  head_dim in {64, 72, 128}
+ *   q_rows, k_rows   rows of q and o, rows of k and v (every room counted)
+ *   max_q, max_k     no document has more query rows, or keys (longer ones
+ *                    are cut to them)
+ *   dtype            of q, k, v and o
+ *   scale > 0;  cap >= 0 (0: none)
+ *   *_row, *_head    strides in elements between rows and between heads of
+ *                    each tensor, multiples of 8 (bf16) or 4 (fp32); the
+ *                    head_dim elements of a head are contiguous.  Rows at
+ *                    most 2^22 elements apart. */
+typedef enum { DIT_MASK_FULL = 0, DIT_MASK_CAUSAL = 1, DIT_MASK_PREFIX = 2 } dit_attn_mask;
+typedef struct {
+  int32_t docs, heads, kv_heads, head_dim;
+  int32_t q_rows, k_rows, max_q, max_k;
+  int32_t dtype, mask;
+  float scale, cap;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+} dit_attn_shape;
+
+/* Bytes of workspace of dit_attention (it may be 0: then pass NULL); -1 cast
+ * to size_t for an invalid shape, dit_last_error() then says why. */
+size_t dit_attention_workspace_bytes(const dit_attn_shape *s);
+
+/*   q_start, k_start  [docs + 1] int32, or NULL for equal rooms of max_q
+ *                     query rows (max_k key rows) each
+ *   k_len             [docs] int32 filled keys of each document, or NULL: all
+ *   prefix            [docs] int32 (DIT_MASK_PREFIX; NULL otherwise)
+ *   slopes            [heads] fp32, or NULL
+ *   workspace         256-byte aligned */
+dit_status dit_attention(const dit_attn_shape *s, const void *q, const void *k, const void *v, void *o,
+                         const int32_t *q_start, const int32_t *k_start, const int32_t *k_len,
+                         const int32_t *prefix, const float *slopes, void *workspace, size_t ws_bytes,
+                         void *stream);
+
+/* 8-bit floating point (OCP e4m3: 448 the largest value, no infinities) with
+ * an fp32 scale for every block of 128 columns, of one row (block_rows = 1:
+ * activations) or of 128 rows (block_rows = 128: weights):
+ *   scale = max(amax / 448, 2^-126),  code = e4m3(x * (1 / scale))
+ * rounded to nearest even; the last blocks of a row or a column may be
+ * partial.  NaN becomes the NaN code, in a block whose scale comes from its
+ * other values; an infinity makes its block's scale infinite.
+ *   x      [rows, cols] of dtype (fp32 or bf16), rows x_row elements apart
+ *   codes  [rows, cols] bytes, contiguous
+ *   scale  [ceil(rows / block_rows), ceil(cols / 128)] fp32
+ *   cols, x_row: multiples of 8;  rows >= 0 */
+dit_status dit_quantize_fp8(int32_t rows, int32_t cols, int32_t block_rows, int32_t dtype, const void *x,
+                            int64_t x_row, void *codes, float *scale, void *stream);
+
+/* A linear layer on such operands:
+ *   y[m, n] = act(sum_k a[m, k] a_scale[m, k/128] * w[n, k] w_scale[n/128, k/128] + bias[n])
+ * A block's products are added before they are scaled: for an fp32 output in
+ * fp32, otherwise on the 8-bit matrix pipe, which adds every 8 consecutive
+ * products aligned to the largest of them with a last place of 2^-13 of its
+ * binade, and those sums in fp32.
+ *   rows >= 0, in a multiple of 16, out >= 1 (a multiple of 8 for DIT_E4M3)
+ *   act    DIT_ACT_NONE, DIT_ACT_GELU (tanh)
+ *   dtype  of out: DIT_F32, DIT_BF16, or DIT_E4M3, which quantises every row
+ *          of y anew in blocks of 128 (as dit_quantize_fp8 with block_rows 1)
+ *          into out and out_scale [rows, ceil(out / 128)] */
+#define DIT_E4M3 2
+typedef enum { DIT_ACT_NONE = 0, DIT_ACT_GELU = 1 } dit_activation;
+typedef struct {
+  int32_t rows, in, out;
+  int32_t act, dtype;
+} dit_linear_shape;
+
+/* As dit_attention_workspace_bytes. */
+size_t dit_linear_fp8_workspace_bytes(const dit_linear_shape *s);
+
+/*   a [rows, in], w [out, in] e4m3 codes; a_scale [rows, ceil(in / 128)],
+ *   w_scale [ceil(out / 128), ceil(in / 128)] fp32; bias [out] or NULL (fp32
+ *   for DIT_F32, else bf16); out [rows, out]; out_scale for DIT_E4M3, else
+ *   NULL.  All contiguous. */
+dit_status dit_linear_fp8(const dit_linear_shape *s, const void *a, const float *a_scale, const void *w,
+                          const float *w_scale, const void *bias, void *out, float *out_scale, void *workspace,
+                          size_t ws_bytes, void *stream);
+
+/* The norms around a sub-layer with its gate and residual, in one pass (the
+ * block with norms before and after each sub-layer):
+ *   x_out = res_scale * x + gate_b * (norm_post(y) * w_post)
+ *   h     = norm_pre(x_out) * w_pre * (1 + scale_b) + shift_b
+ * DIT_NORM_LAYER subtracts the mean and divides by the standard deviation
+ * (biased variance), DIT_NORM_RMS divides by the root mean square, both with
+ * eps; DIT_NORM_NONE (post only) leaves y as it is.  b = row_batch[row].
+ *   rows >= 0, hidden a multiple of 8 in 8 .. 8192
+ *   batch      rows of gate, shift and scale, mod_stride elements apart (a
+ *              multiple of 4): slices of one modulation matrix
+ *   y_dtype    of y: DIT_F32 or DIT_BF16
+ *   h_dtype    of h: DIT_F32, DIT_BF16 or DIT_E4M3 (with h_scale
+ *              [rows, ceil(hidden / 128)], as dit_quantize_fp8, block_rows 1)
+ *   x, x_out   [rows, hidden] fp32; x_out may be x itself
+ *   y          [rows, hidden], or NULL: x_out = res_scale * x (x_out may be
+ *              NULL too: then h is the norm of res_scale * x alone)
+ *   h          [rows, hidden], or NULL: no norm follows
+ *   w_post, w_pre  [hidden] fp32 or NULL (ones);  gate NULL: ones;
+ *   shift, scale   both or neither;  row_batch [rows] int32, or NULL: equal
+ *              samples of rows / batch rows each (rounded up) */
+typedef enum { DIT_NORM_NONE = 0, DIT_NORM_LAYER = 1, DIT_NORM_RMS = 2 } dit_norm_kind;
+typedef struct {
+  int32_t rows, hidden, batch;
+  int32_t post, pre;
+  int32_t y_dtype, h_dtype;
+  float eps, res_scale;
+  int64_t mod_stride;
+} dit_norm_shape;
+dit_status dit_norm_residual(const dit_norm_shape *s, const float *x, float *x_out, const void *y,
+                             const float *w_post, const float *gate, const float *w_pre, const float *shift,
+                             const float *scale, const int32_t *row_batch, void *h, float *h_scale, void *stream);
+
 /* Kernel timing hook for measurement.  dit_timing_enable() (host allocation
  * of HIP events, not a compute call) makes every later launch of kernel class
  * `kclass` record a start/stop hipEvent pair on its launch stream (timing-only

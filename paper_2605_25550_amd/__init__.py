@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("DITMI_LIB") or os.path.join(_HERE, "libditmi.so")
 
 DIT_OK, DIT_ERR_INVALID_ARG, DIT_ERR_UNSUPPORTED, DIT_ERR_WORKSPACE, DIT_ERR_HIP = 0, -1, -2, -3, -4
-DIT_F32, DIT_BF16 = 0, 1
+DIT_F32, DIT_BF16, DIT_E4M3 = 0, 1, 2
 DIT_WS_BLOCK, DIT_WS_STEP, DIT_WS_COND, DIT_WS_SAMPLE, DIT_WS_SERVE = 0, 1, 2, 3, 4
 NOALLOC_SCRATCH_BYTES = 128 << 20  # DIT_NOALLOC_SCRATCH_BYTES of include/ditmi.h
 KERNEL_CLASSES = {"gemm_qkv": 0, "attention": 1, "gemm_out": 2, "gemm_fc1": 3, "gemm_fc2": 4,
@@ -28,6 +28,8 @@ KERNEL_CLASSES = {"gemm_qkv": 0, "attention": 1, "gemm_out": 2, "gemm_fc1": 3, "
 
 STREAM_FIELDS = ("w_ada", "b_ada", "w_qkv", "b_qkv", "w_o", "b_o", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
 C_API = ("dit_workspace_bytes", "dit_block_forward", "dit_block_forward_noalloc", "dit_step_forward", "dit_sample_euler", "dit_serve", "dit_cond_embed", "dit_pos_embed_2d",
+         "dit_attention", "dit_attention_workspace_bytes", "dit_quantize_fp8", "dit_linear_fp8",
+         "dit_linear_fp8_workspace_bytes", "dit_norm_residual",
          "dit_timing_enable", "dit_timing_read", "dit_timing_disable", "dit_status_string", "dit_last_error",
          "dit_version")
 
@@ -70,6 +72,22 @@ class Request(ctypes.Structure):
     _fields_ = [("z_in", ctypes.c_void_p), ("z_out", ctypes.c_void_p), ("y", ctypes.c_void_p), ("cond", ctypes.c_void_p)]
 
 
+class AttnShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("docs", "heads", "kv_heads", "head_dim", "q_rows", "k_rows", "max_q",
+                                              "max_k", "dtype", "mask")] + \
+               [(n, ctypes.c_float) for n in ("scale", "cap")] + \
+               [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "o_row", "o_head")]
+
+
+class LinearShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "in_features", "out_features", "act", "dtype")]
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "hidden", "batch", "post", "pre", "y_dtype", "h_dtype")] + \
+               [("eps", ctypes.c_float), ("res_scale", ctypes.c_float), ("mod_stride", ctypes.c_int64)]
+
+
 def lib() -> ctypes.CDLL:
     """Load libditmi.so (raises if it has not been built)."""
     global _LIB
@@ -91,11 +109,19 @@ def lib() -> ctypes.CDLL:
     L.dit_serve.argtypes = [P(Shape), P(StepWeights), P(CondWeights), P(Request), i32, P(ctypes.c_float), i32,
                             ctypes.c_float, i32, ctypes.c_uint32, ctypes.c_uint32, vp, sz, vp, vp]
     L.dit_pos_embed_2d.argtypes = [i32, i32, i32, vp, vp]
+    L.dit_attention_workspace_bytes.argtypes = [P(AttnShape)]
+    L.dit_attention.argtypes = [P(AttnShape)] + [vp] * 10 + [sz, vp]
+    L.dit_quantize_fp8.argtypes = [i32, i32, i32, i32, vp, ctypes.c_int64, vp, vp, vp]
+    L.dit_linear_fp8_workspace_bytes.argtypes = [P(LinearShape)]
+    L.dit_linear_fp8.argtypes = [P(LinearShape)] + [vp] * 8 + [sz, vp]
+    L.dit_norm_residual.argtypes = [P(NormShape)] + [vp] * 12
+    L.dit_attention_workspace_bytes.restype = L.dit_linear_fp8_workspace_bytes.restype = sz
     L.dit_timing_enable.argtypes = [ctypes.c_int, ctypes.c_int]
     L.dit_timing_read.argtypes = [P(ctypes.c_double), P(ctypes.c_int), P(ctypes.c_double), P(ctypes.c_double)]
     L.dit_timing_disable.argtypes = []
     for fn in ("dit_block_forward", "dit_block_forward_noalloc", "dit_step_forward", "dit_cond_embed", "dit_pos_embed_2d", "dit_timing_enable",
-               "dit_timing_read", "dit_timing_disable"):
+               "dit_timing_read", "dit_timing_disable", "dit_attention", "dit_quantize_fp8", "dit_linear_fp8",
+               "dit_norm_residual"):
         getattr(L, fn).restype = ctypes.c_int
     L.dit_status_string.argtypes = [ctypes.c_int]
     L.dit_status_string.restype = ctypes.c_char_p
@@ -304,6 +330,200 @@ def cond_embed(shape: Shape, t: torch.Tensor, y: torch.Tensor, w: Dict[str, torc
 
 def pos_embed_2d(grid_h: int, grid_w: int, hidden: int, pos: torch.Tensor, stream=None) -> None:
     _check(lib().dit_pos_embed_2d(grid_h, grid_w, hidden, _ptr(pos, torch.float32, "pos"), _stream(stream)))
+
+
+# ---------------------------------------------------------------- stand-alone operators
+_DTYPE_IDS = {torch.float32: DIT_F32, torch.bfloat16: DIT_BF16, torch.float8_e4m3fn: DIT_E4M3}
+_TORCH_DTYPES = (torch.float32, torch.bfloat16, torch.float8_e4m3fn)
+_DTYPE_NAMES = {"f32": DIT_F32, "bf16": DIT_BF16, "e4m3": DIT_E4M3}
+_MASKS = {"full": 0, "causal": 1, "prefix": 2}
+_NORMS = {"none": 0, "layer": 1, "rms": 2}
+_ACTS = {"none": 0, "gelu": 1}
+
+
+def _pick(table, key, what):
+    if key not in table:
+        raise ValueError(f"{what} must be one of {', '.join(table)} (got {key!r})")
+    return table[key]
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The device index that every tensor of a call shares."""
+    i = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != i:
+            raise ValueError(f"tensors on cuda:{i} and {t.device} in one call")
+    return i
+
+
+def _launch(device: int, stream, fn, *args) -> None:
+    """Calls fn(*args, stream) on the tensors' device, whichever is current,
+    and on its current stream unless one is given."""
+    if stream is not None:
+        if stream.device_index != device:
+            raise ValueError(f"the stream is on cuda:{stream.device_index}, the tensors on cuda:{device}")
+        raw = stream.cuda_stream
+    else:
+        raw = torch._C._cuda_getCurrentRawStream(device)
+    if device == torch.cuda.current_device():
+        st = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, raw)
+    _check(st)
+
+
+def _workspace(n: int, device) -> Optional[torch.Tensor]:
+    if n == ctypes.c_size_t(-1).value:
+        raise DitError(DIT_ERR_INVALID_ARG, last_error())
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _strided_ptr(t: torch.Tensor, dtype, shape, name: str, row: int, head: int):
+    """Pointer of a [rows, heads, head_dim] tensor with the strides its shape struct states."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.shape != shape or (t.numel() and (t.stride(2) != 1 or (shape[0] > 1 and t.stride(0) != row) or
+                                           (shape[1] > 1 and t.stride(1) != head))):
+        raise ValueError(f"{name} is {tuple(t.shape)} with strides {t.stride()}; "
+                         f"the shape states {shape} with strides ({row}, {head}, 1)")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    return t.data_ptr()
+
+
+def _sized_ptr(t: Optional[torch.Tensor], dtype, numel: int, name: str):
+    p = _ptr(t, dtype, name)
+    if t is not None and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, the call reads or writes {numel}")
+    return p
+
+
+def attn_shape(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, docs: int, max_q: int, max_k: int,
+               mask: str = "full", scale: Optional[float] = None, cap: float = 0.0) -> AttnShape:
+    """Shape struct of attention calls on tensors laid out as these: q, o
+    [query rows, heads, head_dim], k, v [key rows, kv_heads, head_dim], the last
+    dimension contiguous (views of a fused projection or of a cache).  max_q
+    and max_k bound a document's queries and keys (its room, where no q_start
+    or k_start is given); scale defaults to 1/sqrt(head_dim)."""
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
+        if t.dim() != 3:
+            raise ValueError(f"{name} must be [rows, heads, head_dim] (got {tuple(t.shape)})")
+        if t.dtype != q.dtype or t.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"q, k, v and o must all be float32 or all bfloat16 (got {t.dtype} for {name})")
+    dh = q.shape[2]
+    st = []
+    for t in (q, k, v, o):  # a stride over one element is never used, whatever torch states
+        st += [t.stride(0) if t.shape[0] > 1 else t.shape[1] * dh, t.stride(1) if t.shape[1] > 1 else dh]
+    return AttnShape(docs, q.shape[1], k.shape[1], dh, q.shape[0], k.shape[0], max_q, max_k, _DTYPE_IDS[q.dtype],
+                     _pick(_MASKS, mask, "mask"), dh ** -0.5 if scale is None else scale, cap, *st)
+
+
+def attention_workspace(shape: AttnShape, device="cuda") -> Optional[torch.Tensor]:
+    """Workspace of attention calls of this shape (None where none is needed)."""
+    return _workspace(lib().dit_attention_workspace_bytes(ctypes.byref(shape)), device)
+
+
+def attention(shape: AttnShape, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+              workspace: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+              k_start: Optional[torch.Tensor] = None, k_len: Optional[torch.Tensor] = None,
+              prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Masked attention over documents into o: q_start, k_start [docs + 1], k_len,
+    prefix [docs] int32 and slopes [heads] fp32 on the device."""
+    s = shape
+    dt = _TORCH_DTYPES[s.dtype]
+    i32 = torch.int32
+    qs, ks = (s.q_rows, s.heads, s.head_dim), (s.k_rows, s.kv_heads, s.head_dim)
+    args = (ctypes.byref(s), _strided_ptr(q, dt, qs, "q", s.q_row, s.q_head),
+            _strided_ptr(k, dt, ks, "k", s.k_row, s.k_head), _strided_ptr(v, dt, ks, "v", s.v_row, s.v_head),
+            _strided_ptr(o, dt, qs, "o", s.o_row, s.o_head), _sized_ptr(q_start, i32, s.docs + 1, "q_start"),
+            _sized_ptr(k_start, i32, s.docs + 1, "k_start"), _sized_ptr(k_len, i32, s.docs, "k_len"),
+            _sized_ptr(prefix, i32, s.docs, "prefix"), _sized_ptr(slopes, torch.float32, s.heads, "slopes"),
+            _ptr(workspace, None, "workspace"), 0 if workspace is None else workspace.nbytes)
+    _launch(_same_device(q, k, v, o, q_start, k_start, k_len, prefix, slopes, workspace), stream, lib().dit_attention,
+            *args)
+
+
+def quantize_fp8(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, block_rows: int = 1, stream=None) -> None:
+    """x [rows, cols] (rows may be strided) to e4m3 codes [rows, cols] and fp32
+    scales [ceil(rows / block_rows), ceil(cols / 128)]."""
+    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda:
+        raise ValueError(f"x must be a [rows, cols] float32 or bfloat16 device tensor (got {x.dtype} {tuple(x.shape)})")
+    if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError("x's columns must be contiguous")
+    R, C = x.shape
+    nr = -(-R // block_rows) if block_rows > 0 else 0
+    args = (R, C, block_rows, _DTYPE_IDS[x.dtype], x.data_ptr(), x.stride(0) if R > 1 else C,
+            _sized_ptr(codes, torch.float8_e4m3fn, R * C, "codes"),
+            _sized_ptr(scale, torch.float32, nr * -(-C // 128), "scale"))
+    _launch(_same_device(x, codes, scale), stream, lib().dit_quantize_fp8, *args)
+
+
+def linear_shape(rows: int, in_features: int, out_features: int, act: str = "none", dtype: str = "bf16") -> LinearShape:
+    """Shape struct of linear_fp8: act "none" or "gelu", dtype of the output
+    "bf16", "f32" or "e4m3"."""
+    return LinearShape(rows, in_features, out_features, _pick(_ACTS, act, "act"), _pick(_DTYPE_NAMES, dtype, "dtype"))
+
+
+def linear_fp8_workspace(shape: LinearShape, device="cuda") -> Optional[torch.Tensor]:
+    """Workspace of linear_fp8 calls of this shape (None where none is needed)."""
+    return _workspace(lib().dit_linear_fp8_workspace_bytes(ctypes.byref(shape)), device)
+
+
+def linear_fp8(shape: LinearShape, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+               out: torch.Tensor, workspace: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               out_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out = act(a w^T + bias) on e4m3 codes a [rows, in], w [out, in] with block
+    scales (quantize_fp8 with block_rows 1 and 128); bias fp32 for an fp32
+    output, else bf16; out_scale [rows, ceil(out / 128)] for an e4m3 output."""
+    s = shape
+    M, K, N = s.rows, s.in_features, s.out_features
+    kb, nb = -(-K // 128), -(-N // 128)
+    f8, f32 = torch.float8_e4m3fn, torch.float32
+    args = (ctypes.byref(s), _sized_ptr(a, f8, M * K, "a"), _sized_ptr(a_scale, f32, M * kb, "a_scale"),
+            _sized_ptr(w, f8, N * K, "w"), _sized_ptr(w_scale, f32, nb * kb, "w_scale"),
+            _sized_ptr(bias, f32 if s.dtype == DIT_F32 else torch.bfloat16, N, "bias"),
+            _sized_ptr(out, _TORCH_DTYPES[s.dtype], M * N, "out"), _sized_ptr(out_scale, f32, M * nb, "out_scale"),
+            _ptr(workspace, None, "workspace"), 0 if workspace is None else workspace.nbytes)
+    _launch(_same_device(a, a_scale, w, w_scale, out, workspace, bias, out_scale), stream, lib().dit_linear_fp8, *args)
+
+
+def norm_shape(rows: int, hidden: int, batch: int = 1, post: str = "none", pre: str = "layer", y_dtype: str = "f32",
+               h_dtype: str = "bf16", eps: float = 1e-6, res_scale: float = 1.0, mod_stride: int = 0) -> NormShape:
+    """Shape struct of norm_residual: norms "none" (post only), "layer" or "rms";
+    batch rows of gate, shift and scale, mod_stride elements apart."""
+    return NormShape(rows, hidden, batch, _pick(_NORMS, post, "post"), _pick(_NORMS, pre, "pre"),
+                     _pick(_DTYPE_NAMES, y_dtype, "y_dtype"), _pick(_DTYPE_NAMES, h_dtype, "h_dtype"), eps, res_scale,
+                     mod_stride or hidden)
+
+
+def _mod_ptr(t: Optional[torch.Tensor], s: NormShape, name: str):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (s.batch, s.hidden) or t.stride(1) != 1 or \
+            (s.batch > 1 and t.stride(0) != s.mod_stride) or not t.is_cuda:
+        raise ValueError(f"{name} must be a float32 [{s.batch}, {s.hidden}] device tensor whose rows are {s.mod_stride} "
+                         f"apart (got {t.dtype} {tuple(t.shape)}, strides {t.stride()})")
+    return t.data_ptr()
+
+
+def norm_residual(shape: NormShape, x: torch.Tensor, x_out: Optional[torch.Tensor], h: Optional[torch.Tensor],
+                  y: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None,
+                  shift: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                  row_batch: Optional[torch.Tensor] = None, h_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """x_out = res_scale x + gate norm_post(y), h = norm_pre(x_out) modulated;
+    x_out may be x.  h_scale [rows, ceil(hidden / 128)] for an e4m3 h."""
+    s = shape
+    n, f32 = s.rows * s.hidden, torch.float32
+    args = (ctypes.byref(s), _sized_ptr(x, f32, n, "x"), _sized_ptr(x_out, f32, n, "x_out"),
+            _sized_ptr(y, _TORCH_DTYPES[s.y_dtype], n, "y"), _sized_ptr(w_post, f32, s.hidden, "w_post"),
+            _mod_ptr(gate, s, "gate"), _sized_ptr(w_pre, f32, s.hidden, "w_pre"), _mod_ptr(shift, s, "shift"),
+            _mod_ptr(scale, s, "scale"), _sized_ptr(row_batch, torch.int32, s.rows, "row_batch"),
+            _sized_ptr(h, _TORCH_DTYPES[s.h_dtype], n, "h"),
+            _sized_ptr(h_scale, f32, s.rows * -(-s.hidden // 128), "h_scale"))
+    _launch(_same_device(x, x_out, h, y, w_post, gate, w_pre, shift, scale, row_batch, h_scale), stream,
+            lib().dit_norm_residual, *args)
 
 
 def timing_enable(kclass: str, max_launches: int) -> None:

@@ -16,7 +16,10 @@ LIB = os.path.join(PKG, "libditmi.so")
 OBJDIR = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
-SOURCES = ["gemm_bf16.hip", "gemm_bf16_kg.hip", "gemm_f32.hip", "attention_bf16.hip", "attention_f32.hip", "elementwise.hip", "ditmi.cpp"]
+SOURCES = ["gemm_bf16.hip", "gemm_bf16_kg.hip", "gemm_f32.hip", "attention_bf16.hip", "attention_f32.hip",
+           "elementwise.hip",
+           "attention_doc.hip", "attention_doc_f32.hip", "linear_fp8.hip", "norm_residual.hip", "ditmi.cpp", "operators.cpp"]
+HOST_SOURCES = ["ditmi.cpp", "operators.cpp"]
 PROBE = os.path.join(PKG, "gemm_probe")
 
 # Packed-fp32 instructions are disabled for every device compile.
@@ -102,8 +105,8 @@ def build_hbm_probe() -> str:
 
 
 # Host-code sanitizers for the CPU tests of the C ABI: the host side
-# (ditmi.cpp: validation, workspace layout, tile planning, launch sequencing)
-# is rebuilt with AddressSanitizer and UndefinedBehaviorSanitizer; the kernel
+# (ditmi.cpp and operators.cpp: validation, workspace layout, tile planning,
+# launch sequencing) is rebuilt with AddressSanitizer and UndefinedBehaviorSanitizer; the kernel
 # objects are the regular ones (device code is never sanitized).  The library
 # is loaded into a process that preloads the ASan runtime (sanitizer_runtime()).
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
@@ -127,19 +130,21 @@ def build_sanitized(out_dir: str) -> str:
     """libditmi.so with the host code under ASan + UBSan, in out_dir."""
     os.makedirs(OBJDIR, exist_ok=True)
     os.makedirs(out_dir, exist_ok=True)
-    kernels = [s for s in SOURCES if s != "ditmi.cpp"]
+    kernels = [s for s in SOURCES if s not in HOST_SOURCES]
     objs = [os.path.join(OBJDIR, os.path.splitext(s)[0] + ".o") for s in kernels]
     missing = [s for s, o in zip(kernels, objs) if not os.path.exists(o)]
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         list(ex.map(lambda s: _compile(s, []), missing))
-    host = os.path.join(out_dir, "ditmi_san.o")
-    cmd = [hipcc(), f"--offload-arch={ARCH}", "-O1", "-fPIC", "-std=c++17", "-I", INCLUDE, "-I", CSRC, *DEVICE_FLAGS,
-           *SAN_FLAGS, "-c", os.path.join(CSRC, "ditmi.cpp"), "-o", host]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"sanitized compile failed:\n{r.stdout}{r.stderr}")
+    hosts = []
+    for src in HOST_SOURCES:
+        hosts.append(os.path.join(out_dir, os.path.splitext(src)[0] + "_san.o"))
+        cmd = [hipcc(), f"--offload-arch={ARCH}", "-O1", "-fPIC", "-std=c++17", "-I", INCLUDE, "-I", CSRC, *DEVICE_FLAGS,
+               *SAN_FLAGS, "-c", os.path.join(CSRC, src), "-o", hosts[-1]]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"sanitized compile failed:\n{r.stdout}{r.stderr}")
     lib = os.path.join(out_dir, "libditmi.so")
-    cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *SAN_FLAGS, host, *objs, "-o", lib]
+    cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *SAN_FLAGS, *hosts, *objs, "-o", lib]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"sanitized link failed:\n{r.stdout}{r.stderr}")

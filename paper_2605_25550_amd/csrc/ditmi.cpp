@@ -18,6 +18,7 @@
 #include <vector>
 
 #include "ditmi.h"
+#include "host.h"
 #include "kernels.h"
 
 using namespace ditmi;
@@ -26,18 +27,7 @@ namespace {
 
 thread_local std::string g_err;
 
-dit_status fail(dit_status st, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  g_err = buf;
-  return st;
-}
-
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 inline long rup(long x, long m) { return (x + m - 1) / m * m; }
 
 // ------------------------------------------------------------------ validation
@@ -189,29 +179,6 @@ struct Timing {
   std::vector<hipEvent_t> ev;
   double flops = 0, bytes = 0;
 } g_timing;
-
-template <typename Fn>
-hipError_t timed(int kclass, double flops, double bytes, hipStream_t st, Fn&& launch) {
-  bool rec = false;
-  int slot = 0;
-  {
-    std::lock_guard<std::mutex> lk(g_timing.mu);
-    if (g_timing.kclass == kclass && g_timing.used < g_timing.max) {
-      rec = true;
-      slot = g_timing.used++;
-      g_timing.flops += flops;
-      g_timing.bytes += bytes;
-    }
-  }
-  if (rec) {
-    hipError_t e = hipEventRecord(g_timing.ev[2 * slot], st);
-    if (e != hipSuccess) return e;
-  }
-  hipError_t e = launch();
-  if (e != hipSuccess) return e;
-  if (rec) return hipEventRecord(g_timing.ev[2 * slot + 1], st);
-  return hipSuccess;
-}
 
 // ------------------------------------------------------------------ GEMM planning
 struct Gemm {
@@ -555,12 +522,6 @@ struct StreamIO {
   const float* mod;   // [B, 6D]
   int Ts;             // tokens of this stream per sample
 };
-
-#define HIP_TRY(expr)                                                                     \
-  do {                                                                                    \
-    hipError_t _e = (expr);                                                               \
-    if (_e != hipSuccess) return fail(DIT_ERR_HIP, "%s: %s", #expr, hipGetErrorString(_e)); \
-  } while (0)
 
 // The LayerNorm-modulate of one stream into the operand buffer h, with the
 // modulation vectors shift and scale (stride between samples).
@@ -972,6 +933,34 @@ dit_status scratch_of_stream(hipStream_t hs, char** out) {
 }
 
 }  // namespace
+
+namespace ditmi {
+
+dit_status fail(dit_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return st;
+}
+
+hipError_t timed_begin(int kclass, double flops, double bytes, hipStream_t st, int* slot) {
+  *slot = -1;
+  {
+    std::lock_guard<std::mutex> lk(g_timing.mu);
+    if (g_timing.kclass != kclass || g_timing.used >= g_timing.max) return hipSuccess;
+    *slot = g_timing.used++;
+    g_timing.flops += flops;
+    g_timing.bytes += bytes;
+  }
+  return hipEventRecord(g_timing.ev[2 * *slot], st);
+}
+
+hipError_t timed_end(int slot, hipStream_t st) { return hipEventRecord(g_timing.ev[2 * slot + 1], st); }
+
+}  // namespace ditmi
 
 // ====================================================================== C ABI
 extern "C" {

@@ -121,6 +121,60 @@ struct AdaArgs {
   int B, D;
 };
 
+// ------------------------------------------------------------------ masked attention over documents
+// Document d: query rows [q_start[d], q_start[d+1]), keys k_start[d] + [0, nk).  A row of the kernels'
+// query tiles is (query i, head g of the G = H / Hk heads that share keys), i = r / G, g = r % G, so that
+// the heads sharing keys read them once.  Every mask is a limit per row: keys j < lim(i) are visible.
+struct DocAttnArgs {
+  const void *q, *k, *v;
+  void* o;
+  const int32_t *q_start, *k_start, *k_len, *prefix;  // device arrays or NULL (ditmi.h: dit_attention)
+  const float* slopes;
+  int docs, H, Hk, G;
+  int q_rows, k_rows, max_q, max_k, mask;  // max_*: no document is longer, and none than the tensor
+  int room_q, room_k;                      // rows from one document to the next without q_start / k_start
+  float scale, cap;
+  long q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;  // strides in elements
+  // split > 1: the keys of every item are divided into `split` ranges, whose unnormalised results
+  // go to part[range][query row * H + head][dh + 4] (fp32 O relative to m, m, l) and a merge pass
+  int split;
+  float* part;
+};
+struct DocAttnPlan {
+  int kernel;  // DOC_*
+  int split;
+};
+enum { DOC_ROWS = 0, DOC_SPLIT = 1 };  // waves own rows / waves of a workgroup share 32 rows and divide the keys
+DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype);
+
+// ------------------------------------------------------------------ 8-bit products, block scales of 128
+struct LinF8Args {
+  const uint8_t *a, *w;
+  const float *a_scale, *w_scale;
+  const void* bias;
+  void* out;
+  float* out_scale;
+  int M, N, K, act, dtype;
+  int split;    // k-ranges (of whole blocks) whose fp32 products go to part[range][M][N]
+  float* part;
+};
+// k-ranges that the product is divided into (1: none; their partials take split * M * N * 4 bytes)
+int linear_fp8_split(int M, int N, int K);
+
+// ------------------------------------------------------------------ norms with gate and residual
+struct NormResArgs {
+  const float* x;
+  float* x_out;
+  const void* y;
+  const float *w_post, *gate, *w_pre, *shift, *scale;
+  const int32_t* row_batch;
+  void* h;
+  float* h_scale;
+  int rows, D, batch, per_batch, post, pre, y_dtype, h_dtype;
+  float eps, res_scale;
+  long mod_stride;
+};
+
 // ------------------------------------------------------------------ launchers
 // Each returns hipSuccess or the launch error.  dtype: 0 = fp32, 1 = bf16.
 hipError_t launch_gemm_bf16(const GemmArgs& a, int epi, int tile_cfg, hipStream_t st);
@@ -157,6 +211,13 @@ hipError_t launch_patch_embed(int rows, int T, int P, int D, const float* z, con
 hipError_t launch_pos_embed_2d(int gh, int gw, int D, float* pos, hipStream_t st);
 // z[i] += a * v[i], i < n; n a multiple of 4, both 16-byte aligned
 hipError_t launch_axpy_f32(float* z, const float* v, float a, long n, hipStream_t st);
+hipError_t launch_doc_attn_bf16(const DocAttnArgs& a, const DocAttnPlan& p, int head_dim, hipStream_t st);
+hipError_t launch_doc_attn_f32(const DocAttnArgs& a, const DocAttnPlan& p, int head_dim, hipStream_t st);
+hipError_t launch_doc_attn_merge(const DocAttnArgs& a, int head_dim, int dtype, hipStream_t st);
+hipError_t launch_quantize_fp8(int rows, int cols, int block_rows, int dtype, const void* x, long x_row, void* codes,
+                               float* scale, hipStream_t st);
+hipError_t launch_linear_fp8(const LinF8Args& a, hipStream_t st);
+hipError_t launch_norm_residual(const NormResArgs& a, hipStream_t st);
 
 // Tile configurations of the bf16 GEMM (BM x BN, LDS ring depth).
 enum {
