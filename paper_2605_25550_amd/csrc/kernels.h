@@ -155,11 +155,17 @@ struct LinF8Args {
   void* out;
   float* out_scale;
   int M, N, K, act, dtype;
-  int split;    // k-ranges (of whole blocks) whose fp32 products go to part[range][M][N]
-  float* part;
+  // the first n_full tiles run whole; the k of each of the others is divided into `split` ranges of
+  // whole blocks, whose fp32 partial tiles go to part[range][tile - n_full][rows][columns of a tile]
+  int n_full, split;
+  float* part;  // (few rows with e4m3 outputs: fp32 sums [M][N])
 };
-// k-ranges that the product is divided into (1: none; their partials take split * M * N * 4 bytes)
-int linear_fp8_split(int M, int N, int K);
+struct LinF8Plan {
+  int tile;  // 0: the kernel of few rows; 128, 256: square tiles
+  int n_full, split;
+  size_t bytes;  // of part
+};
+LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype);
 
 // ------------------------------------------------------------------ norms with gate and residual
 struct NormResArgs {
@@ -216,7 +222,7 @@ hipError_t launch_doc_attn_f32(const DocAttnArgs& a, const DocAttnPlan& p, int h
 hipError_t launch_doc_attn_merge(const DocAttnArgs& a, int head_dim, int dtype, hipStream_t st);
 hipError_t launch_quantize_fp8(int rows, int cols, int block_rows, int dtype, const void* x, long x_row, void* codes,
                                float* scale, hipStream_t st);
-hipError_t launch_linear_fp8(const LinF8Args& a, hipStream_t st);
+hipError_t launch_linear_fp8(const LinF8Args& a, int tile, hipStream_t st);
 hipError_t launch_norm_residual(const NormResArgs& a, hipStream_t st);
 
 // Tile configurations of the bf16 GEMM (BM x BN, LDS ring depth).

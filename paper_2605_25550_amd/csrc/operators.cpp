@@ -101,8 +101,7 @@ dit_status check_linear(const dit_linear_shape* s) {
   return DIT_OK;
 }
 size_t linear_bytes(const dit_linear_shape* s) {
-  const int split = s->rows > 0 ? linear_fp8_split(s->rows, s->out, s->in) : 1;
-  return split > 1 ? (size_t)split * s->rows * s->out * 4 : 0;
+  return s->rows > 0 ? linear_fp8_plan(s->rows, s->out, s->in, s->dtype).bytes : 0;
 }
 
 dit_status check_ws(const void* ws, size_t bytes, size_t need) {
@@ -233,12 +232,14 @@ dit_status dit_linear_fp8(const dit_linear_shape* s, const void* a, const float*
   l.K = s->in;
   l.act = s->act;
   l.dtype = s->dtype;
-  l.split = linear_fp8_split(l.M, l.N, l.K);
+  const LinF8Plan p = linear_fp8_plan(l.M, l.N, l.K, l.dtype);
+  l.n_full = p.n_full;
+  l.split = p.split;
   l.part = (float*)workspace;
   const hipStream_t st = (hipStream_t)stream;
   const double M = l.M, N = l.N, K = l.K;
   HIP_TRY(timed(DIT_K_OTHER, 2 * M * N * K, M * K + N * K + M * N * (l.dtype == 0 ? 4 : l.dtype == 1 ? 2 : 1), st,
-                [&]() { return launch_linear_fp8(l, st); }));
+                [&]() { return launch_linear_fp8(l, p.tile, st); }));
   return DIT_OK;
 }
 
