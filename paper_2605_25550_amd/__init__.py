@@ -347,13 +347,40 @@ def _pick(table, key, what):
     return table[key]
 
 
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
-    """The device index that every tensor of a call shares."""
-    i = first.get_device()
-    for t in others:
-        if t is not None and t.get_device() != i:
-            raise ValueError(f"tensors on cuda:{i} and {t.device} in one call")
-    return i
+def _refuse(t, dtype, numel: Optional[int], name: str, device: int):
+    """The error of a tensor that _arg did not take."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    if t.get_device() != device:
+        raise ValueError(f"tensors on cuda:{device} and {t.device} in one call")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
+    raise ValueError(f"{name} has {t.numel()} elements, the call reads or writes {numel}")
+
+
+def _arg(t: Optional[torch.Tensor], dtype, numel: int, name: str, device: int):
+    """Pointer of a contiguous tensor of that type, size and device (None stays
+    None).  Small calls are bound by the host: one test, and the reasons apart."""
+    if t is None:
+        return None
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.numel() == numel and t.is_contiguous() and device >= 0:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _refuse(t, dtype, numel, name, device)
+
+
+def _ws_arg(t: Optional[torch.Tensor], device: int):
+    if t is None:
+        return None, 0
+    if device < 0 or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, None, None, "workspace", device)
+    return t.data_ptr(), t.nbytes
 
 
 def _launch(device: int, stream, fn, *args) -> None:
@@ -365,7 +392,7 @@ def _launch(device: int, stream, fn, *args) -> None:
         raw = stream.cuda_stream
     else:
         raw = torch._C._cuda_getCurrentRawStream(device)
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         st = fn(*args, raw)
     else:
         with torch.cuda.device(device):
@@ -379,24 +406,17 @@ def _workspace(n: int, device) -> Optional[torch.Tensor]:
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
-def _strided_ptr(t: torch.Tensor, dtype, shape, name: str, row: int, head: int):
+def _strided_ptr(t: torch.Tensor, dtype, shape, name: str, row: int, head: int, device: int):
     """Pointer of a [rows, heads, head_dim] tensor with the strides its shape struct states."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
-    if t.shape != shape or (t.numel() and (t.stride(2) != 1 or (shape[0] > 1 and t.stride(0) != row) or
-                                           (shape[1] > 1 and t.stride(1) != head))):
+    r, h, d = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.shape != shape or (t.numel() and (d != 1 or (r != row and shape[0] > 1) or (h != head and shape[1] > 1))):
         raise ValueError(f"{name} is {tuple(t.shape)} with strides {t.stride()}; "
                          f"the shape states {shape} with strides ({row}, {head}, 1)")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    if device < 0 or t.get_device() != device:
+        _refuse(t, dtype, None, name, device)
     return t.data_ptr()
-
-
-def _sized_ptr(t: Optional[torch.Tensor], dtype, numel: int, name: str):
-    p = _ptr(t, dtype, name)
-    if t is not None and t.numel() != numel:
-        raise ValueError(f"{name} has {t.numel()} elements, the call reads or writes {numel}")
-    return p
 
 
 def attn_shape(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, docs: int, max_q: int, max_k: int,
@@ -431,17 +451,15 @@ def attention(shape: AttnShape, q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     """Masked attention over documents into o: q_start, k_start [docs + 1], k_len,
     prefix [docs] int32 and slopes [heads] fp32 on the device."""
     s = shape
-    dt = _TORCH_DTYPES[s.dtype]
-    i32 = torch.int32
-    qs, ks = (s.q_rows, s.heads, s.head_dim), (s.k_rows, s.kv_heads, s.head_dim)
-    args = (ctypes.byref(s), _strided_ptr(q, dt, qs, "q", s.q_row, s.q_head),
-            _strided_ptr(k, dt, ks, "k", s.k_row, s.k_head), _strided_ptr(v, dt, ks, "v", s.v_row, s.v_head),
-            _strided_ptr(o, dt, qs, "o", s.o_row, s.o_head), _sized_ptr(q_start, i32, s.docs + 1, "q_start"),
-            _sized_ptr(k_start, i32, s.docs + 1, "k_start"), _sized_ptr(k_len, i32, s.docs, "k_len"),
-            _sized_ptr(prefix, i32, s.docs, "prefix"), _sized_ptr(slopes, torch.float32, s.heads, "slopes"),
-            _ptr(workspace, None, "workspace"), 0 if workspace is None else workspace.nbytes)
-    _launch(_same_device(q, k, v, o, q_start, k_start, k_len, prefix, slopes, workspace), stream, lib().dit_attention,
-            *args)
+    dt, i32, dev = _TORCH_DTYPES[s.dtype], torch.int32, q.get_device()
+    docs, H, dh = s.docs, s.heads, s.head_dim
+    qs, ks = (s.q_rows, H, dh), (s.k_rows, s.kv_heads, dh)
+    ws, n = _ws_arg(workspace, dev)
+    _launch(dev, stream, lib().dit_attention, ctypes.byref(s), _strided_ptr(q, dt, qs, "q", s.q_row, s.q_head, dev),
+            _strided_ptr(k, dt, ks, "k", s.k_row, s.k_head, dev), _strided_ptr(v, dt, ks, "v", s.v_row, s.v_head, dev),
+            _strided_ptr(o, dt, qs, "o", s.o_row, s.o_head, dev), _arg(q_start, i32, docs + 1, "q_start", dev),
+            _arg(k_start, i32, docs + 1, "k_start", dev), _arg(k_len, i32, docs, "k_len", dev),
+            _arg(prefix, i32, docs, "prefix", dev), _arg(slopes, torch.float32, H, "slopes", dev), ws, n)
 
 
 def quantize_fp8(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, block_rows: int = 1, stream=None) -> None:
@@ -452,11 +470,10 @@ def quantize_fp8(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, bloc
     if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
         raise ValueError("x's columns must be contiguous")
     R, C = x.shape
-    nr = -(-R // block_rows) if block_rows > 0 else 0
-    args = (R, C, block_rows, _DTYPE_IDS[x.dtype], x.data_ptr(), x.stride(0) if R > 1 else C,
-            _sized_ptr(codes, torch.float8_e4m3fn, R * C, "codes"),
-            _sized_ptr(scale, torch.float32, nr * -(-C // 128), "scale"))
-    _launch(_same_device(x, codes, scale), stream, lib().dit_quantize_fp8, *args)
+    nr, dev = -(-R // block_rows) if block_rows > 0 else 0, x.get_device()
+    _launch(dev, stream, lib().dit_quantize_fp8, R, C, block_rows, _DTYPE_IDS[x.dtype], x.data_ptr(),
+            x.stride(0) if R > 1 else C, _arg(codes, torch.float8_e4m3fn, R * C, "codes", dev),
+            _arg(scale, torch.float32, nr * -(-C // 128), "scale", dev))
 
 
 def linear_shape(rows: int, in_features: int, out_features: int, act: str = "none", dtype: str = "bf16") -> LinearShape:
@@ -479,13 +496,13 @@ def linear_fp8(shape: LinearShape, a: torch.Tensor, a_scale: torch.Tensor, w: to
     s = shape
     M, K, N = s.rows, s.in_features, s.out_features
     kb, nb = -(-K // 128), -(-N // 128)
-    f8, f32 = torch.float8_e4m3fn, torch.float32
-    args = (ctypes.byref(s), _sized_ptr(a, f8, M * K, "a"), _sized_ptr(a_scale, f32, M * kb, "a_scale"),
-            _sized_ptr(w, f8, N * K, "w"), _sized_ptr(w_scale, f32, nb * kb, "w_scale"),
-            _sized_ptr(bias, f32 if s.dtype == DIT_F32 else torch.bfloat16, N, "bias"),
-            _sized_ptr(out, _TORCH_DTYPES[s.dtype], M * N, "out"), _sized_ptr(out_scale, f32, M * nb, "out_scale"),
-            _ptr(workspace, None, "workspace"), 0 if workspace is None else workspace.nbytes)
-    _launch(_same_device(a, a_scale, w, w_scale, out, workspace, bias, out_scale), stream, lib().dit_linear_fp8, *args)
+    f8, f32, dev = torch.float8_e4m3fn, torch.float32, a.get_device()
+    ws, n = _ws_arg(workspace, dev)
+    _launch(dev, stream, lib().dit_linear_fp8, ctypes.byref(s), _arg(a, f8, M * K, "a", dev),
+            _arg(a_scale, f32, M * kb, "a_scale", dev), _arg(w, f8, N * K, "w", dev),
+            _arg(w_scale, f32, nb * kb, "w_scale", dev),
+            _arg(bias, f32 if s.dtype == DIT_F32 else torch.bfloat16, N, "bias", dev),
+            _arg(out, _TORCH_DTYPES[s.dtype], M * N, "out", dev), _arg(out_scale, f32, M * nb, "out_scale", dev), ws, n)
 
 
 def norm_shape(rows: int, hidden: int, batch: int = 1, post: str = "none", pre: str = "layer", y_dtype: str = "f32",
@@ -497,13 +514,15 @@ def norm_shape(rows: int, hidden: int, batch: int = 1, post: str = "none", pre: 
                      mod_stride or hidden)
 
 
-def _mod_ptr(t: Optional[torch.Tensor], s: NormShape, name: str):
+def _mod_ptr(t: Optional[torch.Tensor], batch: int, hidden: int, stride: int, name: str, device: int):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.shape != (s.batch, s.hidden) or t.stride(1) != 1 or \
-            (s.batch > 1 and t.stride(0) != s.mod_stride) or not t.is_cuda:
-        raise ValueError(f"{name} must be a float32 [{s.batch}, {s.hidden}] device tensor whose rows are {s.mod_stride} "
-                         f"apart (got {t.dtype} {tuple(t.shape)}, strides {t.stride()})")
+    if t.dtype is not torch.float32 or t.shape != (batch, hidden) or t.stride(1) != 1 or \
+            (batch > 1 and t.stride(0) != stride):
+        raise ValueError(f"{name} must be a float32 [{batch}, {hidden}] tensor whose rows are {stride} apart "
+                         f"(got {t.dtype} {tuple(t.shape)}, strides {t.stride()})")
+    if device < 0 or t.get_device() != device:
+        _refuse(t, torch.float32, None, name, device)
     return t.data_ptr()
 
 
@@ -515,15 +534,14 @@ def norm_residual(shape: NormShape, x: torch.Tensor, x_out: Optional[torch.Tenso
     """x_out = res_scale x + gate norm_post(y), h = norm_pre(x_out) modulated;
     x_out may be x.  h_scale [rows, ceil(hidden / 128)] for an e4m3 h."""
     s = shape
-    n, f32 = s.rows * s.hidden, torch.float32
-    args = (ctypes.byref(s), _sized_ptr(x, f32, n, "x"), _sized_ptr(x_out, f32, n, "x_out"),
-            _sized_ptr(y, _TORCH_DTYPES[s.y_dtype], n, "y"), _sized_ptr(w_post, f32, s.hidden, "w_post"),
-            _mod_ptr(gate, s, "gate"), _sized_ptr(w_pre, f32, s.hidden, "w_pre"), _mod_ptr(shift, s, "shift"),
-            _mod_ptr(scale, s, "scale"), _sized_ptr(row_batch, torch.int32, s.rows, "row_batch"),
-            _sized_ptr(h, _TORCH_DTYPES[s.h_dtype], n, "h"),
-            _sized_ptr(h_scale, f32, s.rows * -(-s.hidden // 128), "h_scale"))
-    _launch(_same_device(x, x_out, h, y, w_post, gate, w_pre, shift, scale, row_batch, h_scale), stream,
-            lib().dit_norm_residual, *args)
+    R, D, B, st, f32, dev = s.rows, s.hidden, s.batch, s.mod_stride, torch.float32, x.get_device()
+    n = R * D
+    _launch(dev, stream, lib().dit_norm_residual, ctypes.byref(s), _arg(x, f32, n, "x", dev),
+            _arg(x_out, f32, n, "x_out", dev), _arg(y, _TORCH_DTYPES[s.y_dtype], n, "y", dev),
+            _arg(w_post, f32, D, "w_post", dev), _mod_ptr(gate, B, D, st, "gate", dev), _arg(w_pre, f32, D, "w_pre", dev),
+            _mod_ptr(shift, B, D, st, "shift", dev), _mod_ptr(scale, B, D, st, "scale", dev),
+            _arg(row_batch, torch.int32, R, "row_batch", dev), _arg(h, _TORCH_DTYPES[s.h_dtype], n, "h", dev),
+            _arg(h_scale, f32, R * -(-D // 128), "h_scale", dev))
 
 
 def timing_enable(kclass: str, max_launches: int) -> None:

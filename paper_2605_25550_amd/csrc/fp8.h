@@ -6,24 +6,23 @@ namespace ditmi {
 
 constexpr float F8_MAX = 448.f, F8_TINY = 1.17549435e-38f;  // 2^-126: the least scale
 
-
 __device__ __forceinline__ float f8_scale(float amax) { return fmaxf(amax * (1.0f / F8_MAX), F8_TINY); }
-// Four values to e4m3 codes.  x * inv is at most a rounding above 448, which
-// the conversion would turn into NaN from 464 on; the clamp keeps NaN.
-__device__ __forceinline__ float f8_clamp(float x) { return x > F8_MAX ? F8_MAX : x < -F8_MAX ? -F8_MAX : x; }
+// Four values to e4m3 codes.  The conversion makes NaN of values from 464 on;
+// x / scale exceeds 448 by a rounding at most.
 __device__ __forceinline__ uint32_t pack_f8x4(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(f8_clamp(a), f8_clamp(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f8_clamp(c), f8_clamp(d), w, true);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
+// Eight values that are read once: streamed past the caches.
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
-    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+    const f32x4 a = __builtin_nontemporal_load((const f32x4*)p), b = __builtin_nontemporal_load((const f32x4*)(p + 4));
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
   } else {
-    const u32x4 w = *(const u32x4*)p;
+    const u32x4 w = __builtin_nontemporal_load((const u32x4*)p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }

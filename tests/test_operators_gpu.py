@@ -336,7 +336,8 @@ def test_linear_nan_stays_in_its_row_and_column():
 
 
 # ---------------------------------------------------------------- norms
-@pytest.mark.parametrize("R,D", [(1, 8), (5, 64), (77, 1152), (3, 1160), (130, 2048), (9, 2056), (33, 4096), (4, 4104), (2, 8192), (7, 8)])
+@pytest.mark.parametrize("R,D", [(1, 8), (5, 64), (77, 1152), (3, 1160), (130, 2048), (9, 2056), (33, 4096), (4, 4104), (2, 8192), (7, 8), (2050, 8), (2051, 1160), (2048, 2056),
+                                 (2049, 4096)])
 @pytest.mark.parametrize("post,pre,ydt,hdt", [("none", "layer", "f32", "bf16"), ("layer", "layer", "bf16", "f32"), ("rms", "rms", "bf16", "e4m3"),
                                               ("rms", "layer", "f32", "e4m3")])
 def test_norm_residual(R, D, post, pre, ydt, hdt):
