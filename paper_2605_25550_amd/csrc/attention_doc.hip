@@ -1,6 +1,25 @@
 // Masked attention over documents, bf16: packed or padded documents, key
 // lengths, causal and prefix masks, scores capped by a tanh or biased by the
 // distance, heads that share keys (ditmi.h: dit_attention).
+//
+// Orientation and schedule are those of the block's attention: a wave owns 32
+// rows (query, head of the group that shares keys) and computes S^T = K Q^T with
+// v_mfma_f32_32x32x16_bf16, so that a lane holds scores of one row, then
+// O^T += V^T P^T with the probabilities as they lie; K and V tiles of 64 keys go
+// HBM -> LDS by DMA into a ring of four slots, two to three tiles ahead.  What
+// differs: the tensors are the caller's (token-major, strided), so V^T comes from
+// V's rows by the transposing LDS read (ds_read_b64_tr_b16: of each 16 lanes,
+// lane l addresses 8 bytes of row l / 4 and receives column l of the four rows),
+// and the scale is applied in fp32 to the scores.
+//
+// Every mask is a limit per row, keys j < lim.  Tiles that every row of the
+// workgroup sees whole run software-pipelined: the QK^T MFMAs of tile j + 1 are
+// issued between the exponentials of tile j, its PV MFMAs between the row maxima
+// of tile j + 1.  The few others (the last of a document, those on the diagonal)
+// run one after the other, with the limits applied.
+//
+// The running max moves only when a tile exceeds it by more than 2^64:
+// probabilities then stay exactly representable, and the rescale is rare.
 #include <algorithm>
 
 #include "common.h"
@@ -19,11 +38,13 @@ struct DocCfg {
   static constexpr int CPR = ROW / 16;           // 16-byte chunks per row ...
   static constexpr int RC = DH / 8;              // ... of which hold data
   static constexpr int TILE = BKV * ROW;         // bytes of a K or V tile
-  static constexpr int SLOT = 2 * TILE;
   static constexpr int DT = (DH + 31) / 32;      // 32-row tiles of O^T
   static constexpr int KS = DHP / 16;
   static constexpr int DMA = TILE / 1024;        // DMA instructions of a K or V tile
-  static constexpr int STAGES = 3;
+  static constexpr int ST = 4;                   // ring slots: the K tiles of all, then the V tiles
+  // head_dim 72: V's pad column 72 holds ones, so that O^T row 72 is the row sum
+  static constexpr bool FOLD = CPR > RC;
+  static constexpr int LT = DH / 32, LG = (DH % 32) % 8 / 4, LE = (DH % 32) / 8 * 4 + DH % 4;
   // stored position of 16-byte chunk c of K row r / V row r
   static __device__ __forceinline__ int pos_k(int r, int c) {
     return c ^ (DHP == 128 ? (r & 15) : (DHP == 64 ? ((r >> 1) & 7) : ((r >> 3) & 1)));
@@ -33,19 +54,26 @@ struct DocCfg {
   static __device__ __forceinline__ int pos_v(int r, int c) {
     return c ^ (DHP == 128 ? (r & 3) << 2 : (DHP == 64 ? ((r >> 1) & 1) << 2 : 0));
   }
-  static_assert(TILE % 1024 == 0, "tiles are whole 1 KB DMA blocks");
+  static_assert(TILE % 1024 == 0 && ST * TILE <= 65536, "whole DMA blocks; slot offsets fit the LDS immediate");
 };
 
-template <int DH, int NW, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NW * 64) void doc_attn_bf16_kernel(DocAttnArgs a) {
-  using C = DocCfg<DH>;
-  constexpr int BM = NW * 32;
-  constexpr int IPW = (2 * C::DMA + NW - 1) / NW;
-  // ring of slots, then a line that absorbs spare DMAs (and what transposed
-  // reads of head_dim 72 touch past the last V row)
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::STAGES * C::SLOT + 1024];
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+__device__ __forceinline__ s16x4 read_tr(const lds_byte* p) {
+  typedef __attribute__((address_space(3))) s16x4* lds_p;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p);
+}
 
+template <int DH, int NW, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a) {
+  using C = DocCfg<DH>;
+  constexpr int ST = C::ST, BM = NW * 32;
+  constexpr int IPW = (2 * C::DMA + NW - 1) / NW;  // DMA instructions per wave and tile (uniform)
+  constexpr bool SPARE = IPW * NW > 2 * C::DMA;
+  // the ring, then a line that absorbs spare DMAs (and what transposed reads of
+  // head_dim 72 touch past the last V row)
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * ST * C::TILE + 1024];
   __shared__ int bad[3][DH];
+
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r32 = lane & 31;
@@ -54,9 +82,10 @@ __global__ __launch_bounds__(NW * 64) void doc_attn_bf16_kernel(DocAttnArgs a) {
   const int nqb = (rows + BM - 1) / BM;
   const int items = nqb * a.Hk;
   if ((int)blockIdx.x >= items) return;
+  // query blocks of a head in contiguous ranges per XCD: they share its K and V
+  // in that XCD's L2; heaviest first where later queries see more keys
   const int item = xcd_remap(blockIdx.x, items);
   const int hk = item / nqb;
-  // heaviest query blocks first where later queries see more keys
   const int qb = a.mask ? nqb - 1 - item % nqb : item % nqb;
   const int r0 = qb * BM + wave * 32;                     // first row of this wave
   const int row = min(r0 + r32, rows - 1);                // lanes past the end repeat the last row
@@ -68,6 +97,7 @@ __global__ __launch_bounds__(NW * 64) void doc_attn_bf16_kernel(DocAttnArgs a) {
   const int nkv_all = (lim_hi + C::BKV - 1) / C::BKV;
   const int part = blockIdx.z;
   const int t0 = (int)((long)nkv_all * part / a.split), t1 = (int)((long)nkv_all * (part + 1) / a.split);
+  const int tf = max(t0, min(t1, lim_lo / C::BKV));       // tiles [t0, tf) are seen whole
 
   const bf16_t* __restrict__ kp = (const bf16_t*)a.k + (long)doc.k0 * a.k_row + hk * a.k_head;
   const bf16_t* __restrict__ vp = (const bf16_t*)a.v + (long)doc.k0 * a.v_row + hk * a.v_head;
@@ -80,159 +110,275 @@ __global__ __launch_bounds__(NW * 64) void doc_attn_bf16_kernel(DocAttnArgs a) {
     qf[s] = s * 16 + g * 8 < DH ? *(const bf16x8*)(qp + s * 16 + g * 8) : bf16x8{};
 
   // DMA of one tile into its slot: instruction i < DMA covers K bytes
-  // [1024 i, +1024), the next DMA the V bytes.  The pad chunk of head_dim 72's
-  // rows is no lane's: it keeps the zeros written below.
-  auto issue = [&](int tile) {
-    const unsigned base = lds0 + (unsigned)((tile % C::STAGES) * C::SLOT);
+  // [1024 i, +1024), the next DMA the V bytes; wave w issues i = w + NW t.  The
+  // source is a scalar base (the tile's first row) plus a 32-bit lane offset;
+  // the last tile's rows past the document's end repeat its last row.  The pad
+  // chunk of head_dim 72's rows is no lane's: it keeps what is written below.
+  // Past the last tile, and for spare instructions, the copy goes to the spare
+  // line, so that every wave counts the same.
+  auto issue_one = [&](int tile, int slot, int t) {
+    const int i = wave + NW * t;  // wave-uniform
+    const bool real = !SPARE || i < 2 * C::DMA, isv = real && i >= C::DMA;
     const int kv0 = min(tile, t1 - 1) * C::BKV;
-#pragma unroll
-    for (int t = 0; t < IPW; ++t) {
-      const int qi_ = wave + NW * t;
-      if (qi_ < 2 * C::DMA) {
-        const bool isv = qi_ >= C::DMA;
-        const int byte = (isv ? qi_ - C::DMA : qi_) * 1024 + lane * 16;
-        const int R = byte / C::ROW, pos = (byte % C::ROW) >> 4;
-        const int c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
-        const long key = min(kv0 + R, doc.nk - 1);
-        const bf16_t* src = isv ? vp + key * a.v_row + c * 8 : kp + key * a.k_row + c * 8;
-        if (c < C::RC) dma_16(src, base + (unsigned)(qi_ * 1024));
-      }
-    }
+    const int byte = (isv ? i - C::DMA : real ? i : 0) * 1024 + lane * 16;
+    const int R = byte / C::ROW, pos = (byte % C::ROW) >> 4;
+    const int c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
+    const long rs = isv ? a.v_row : a.k_row;
+    const bf16_t* base = (isv ? vp : kp) + kv0 * rs;
+    const unsigned off = (unsigned)min(R, doc.nk - 1 - kv0) * (unsigned)(rs * 2) + c * 16;
+    const unsigned dst = real && tile < t1 ? lds0 + (isv ? (ST + slot) * C::TILE + (i - C::DMA) * 1024 : slot * C::TILE + i * 1024)
+                                           : lds0 + 2 * ST * C::TILE;
+    if (C::CPR == C::RC || c < C::RC) dma_16s(base, off, dst);
   };
   for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
-  if (C::CPR > C::RC) {
-    for (int e = tid; e < 256; e += NW * 64) ((uint32_t*)(smem + C::STAGES * C::SLOT))[e] = 0;
-    for (int e = tid; e < C::STAGES * 2 * C::BKV * 4; e += NW * 64) {
-      const int R = (e >> 2) & (C::BKV - 1), half = e >> 2 >> 6;  // K or V tile of a slot
-      const int pos = half & 1 ? C::pos_v(R, C::RC) : C::pos_k(R, C::RC);
-      ((uint32_t*)(smem + half * C::TILE + R * C::ROW + pos * 16))[e & 3] = 0;
+  if (C::FOLD) {
+    for (int e = tid; e < 256; e += NW * 64) ((uint32_t*)(smem + 2 * ST * C::TILE))[e] = 0;
+    for (int e = tid; e < 2 * ST * C::BKV * 4; e += NW * 64) {
+      const int R = (e >> 2) & (C::BKV - 1), tile = e >> 8;  // K tiles, then V tiles
+      const int pos = tile >= ST ? C::pos_v(R, C::RC) : C::pos_k(R, C::RC);
+      ((uint32_t*)(smem + tile * C::TILE + R * C::ROW + pos * 16))[e & 3] = tile >= ST && (e & 3) == 0 ? 0x3F80u : 0u;
     }
   }
 
-  int k_off[C::KS];
+  const lds_byte* k_at[C::KS];
 #pragma unroll
-  for (int s = 0; s < C::KS; ++s) k_off[s] = r32 * C::ROW + (C::pos_k(r32, 2 * s + g) << 4);
-  // transposed reads: of each 16-lane group lane l addresses 8 bytes of row
-  // l / 4 and receives column l of the four rows (keys 4 g .. 4 g + 3)
-  int v_off[C::DT];
+  for (int s = 0; s < C::KS; ++s) k_at[s] = (const lds_byte*)smem + r32 * C::ROW + (C::pos_k(r32, 2 * s + g) << 4);
+  const lds_byte* v_at[C::DT];
   {
     const int R = 4 * g + ((lane & 15) >> 2), half = (lane >> 4) & 1;
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
-      v_off[t] = C::TILE + R * C::ROW + (C::pos_v(R, t * 4 + half * 2 + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
+      v_at[t] = (const lds_byte*)smem + ST * C::TILE + R * C::ROW +
+                (C::pos_v(R, t * 4 + half * 2 + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
   }
+  auto kread = [&](int slot, int kt, int s) {
+    return *(const __attribute__((address_space(3))) bf16x8*)(k_at[s] + slot * C::TILE + kt * 32 * C::ROW);
+  };
+  // keys 16 c + 4 g + 0..3 and 16 c + 8 + 4 g + 0..3 of column 32 t + r32: the
+  // keys of the lane's probabilities
+  auto vread = [&](int slot, int c, int t) {
+    const lds_byte* p = v_at[t] + slot * C::TILE + c * 16 * C::ROW;
+    const u32x2 lo = __builtin_bit_cast(u32x2, read_tr(p)), hi = __builtin_bit_cast(u32x2, read_tr(p + 8 * C::ROW));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  };
 
+  // A score goes raw -> z (the exponent in the exp2 domain).  The scale and the
+  // cap keep the order of scores, so that they can wait for the exponential,
+  // after the row max; the bias cannot.
   const float sc = a.scale * LOG2E;
   const float cap_in = CAP ? 2.0f * sc / a.cap : 0.f, cap_out = CAP ? a.cap * LOG2E : 0.f;
   const float slope = BIAS ? a.slopes[h] * LOG2E : 0.f;
-  const int here = qi + doc.nk - doc.nq;
+  const float here = (float)(qi + doc.nk - doc.nq);
+  auto capped = [&](float s) {  // cap tanh(s scale / cap), in the exp2 domain
+    return fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * cap_in) + 1.0f), cap_out);
+  };
+  // before the max: element e of half kt of a tile whose first key, less 4 g, is
+  // `first` keys behind the row's own place
+  auto pre = [&](float s, float first, int kt, int e) {
+    if (!BIAS) return s;
+    const float z = CAP ? capped(s) : s * sc;
+    return fmaf(-slope, fabsf(first - (float)(kt * 32 + (e >> 2) * 8 + (e & 3))), z);
+  };
+  auto z_of_max = [&](float m) { return BIAS ? m : CAP ? capped(m) : m * sc; };
+  float m_run = -INFINITY, mneg = 0.f;  // mneg = -m_run, 0 while nothing has been seen
+  auto prob = [&](float s) {
+    if (BIAS) return __builtin_amdgcn_exp2f(s + mneg);
+    if (CAP)
+      return __builtin_amdgcn_exp2f(
+          fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * cap_in) + 1.0f), cap_out + mneg));
+    return __builtin_amdgcn_exp2f(fmaf(s, sc, mneg));
+  };
   const float TAU = 64.0f;
-  // V values that are not finite, in tiles that some row does not see whole:
-  // a product would bring them to the other rows too (0 * inf).  They are
-  // taken out of LDS, and bad[class][column] keeps the first key of each
-  // class (NaN, +inf, -inf); the rows whose limit lies behind it get theirs
-  // at the end.
-  auto clean_v = [&](int tile) {
-    unsigned char* vt = smem + (tile % C::STAGES) * C::SLOT + C::TILE;
+  // Row sums of the bf16 probabilities (the values the PV product multiplies) on
+  // the matrix pipe: a 4x4x4 MFMA with ones adds the four of a lane's operand.
+  f32x4 lacc = f32x4{};
+  typedef short i16x4 __attribute__((ext_vector_type(4)));
+  const i16x4 ones4 = {0x3F80, 0x3F80, 0x3F80, 0x3F80};
+  auto add_sum = [&](uint32_t w0, uint32_t w1) {
+    if (!C::FOLD) lacc = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_bit_cast(i16x4, u32x2{w0, w1}), lacc, 0, 0, 0);
+  };
+  f32x16 oacc[C::DT];
+#pragma unroll
+  for (int t = 0; t < C::DT; ++t) oacc[t] = f32x16{};
+  auto pv = [&](const u32x4& v, const u32x4& p, int t) {
+    oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), oacc[t], 0, 0, 0);
+  };
+  // moves the running max to that of a tile (z domain, whole row) where it leads by more than 2^TAU
+  auto lead = [&](float z) {
+    if (__builtin_amdgcn_ballot_w64(z > m_run + TAU) == 0) return;
+    const float m_new = fmaxf(m_run, z);
+    // nothing seen so far: O and l are zero, any finite factor will do
+    const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+    lacc *= alpha;
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t) oacc[t] *= alpha;
+    m_run = m_new;
+    mneg = m_new == -INFINITY ? 0.f : -m_new;
+  };
+
+  if (t0 < t1)
+#pragma unroll
+    for (int d = 0; d < ST - 1; ++d)
+#pragma unroll
+      for (int t = 0; t < IPW; ++t) issue_one(t0 + d, d, t);
+
+  if (t0 < tf) {
+    wait_vmcnt<(ST - 3) * IPW>();
+    __syncthreads();
+    f32x16 sa[2], sb[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      sa[kt] = f32x16{};
+#pragma unroll
+      for (int s = 0; s < C::KS; ++s) sa[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(0, kt, s), qf[s], sa[kt], 0, 0, 0);
+    }
+    float mcur = -INFINITY;  // row max of the current tile (what pre() gives), both halves
+    {
+      const float first = here - (float)(t0 * C::BKV + 4 * g);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          sa[kt][e] = pre(sa[kt][e], first, kt, e);
+          mcur = fmaxf(mcur, sa[kt][e]);
+        }
+      mcur = max_halves(mcur);
+    }
+    // One key tile: the exponentials of scur (tile j, slot sj) beside the QK^T
+    // MFMAs of tile j + 1 into snext, then the PV MFMAs of tile j beside the row
+    // max of tile j + 1 and the DMA of tile j + 3.  (The last tile's QK^T reads
+    // the slot behind it: computed, and not used.)
+    auto tile_step = [&](const int j, const int sj, f32x16 (&scur)[2], f32x16 (&snext)[2]) __attribute__((always_inline)) {
+      lead(z_of_max(mcur));
+      constexpr int EX = C::FOLD ? 16 : 24;  // exponentials beside QK^T; the rest beside the first PV MFMAs
+      constexpr int NP = 4 * C::DT, NPRE = EX / 8 * C::DT, ND = 3, NQ = 2 * C::KS;
+      u32x4 pw[4], vf[3];
+      auto pack = [&](int p) { pw[p >> 2][p & 3] = pack_bf16x2(scur[p >> 3][(2 * p) & 15], scur[p >> 3][(2 * p + 1) & 15]); };
+      {
+        const int sl = (sj + 1) % ST;
+        bf16x8 kf[3];
+        kf[0] = kread(sl, 0, 0);
+        kf[1] = kread(sl, 1, 0);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          if (i + 2 < NQ) kf[(i + 2) % 3] = kread(sl, (i + 2) & 1, (i + 2) >> 1);
+          snext[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % 3], qf[i >> 1], i < 2 ? f32x16{} : snext[i & 1], 0, 0, 0);
+          if (i == NQ - 2) vf[0] = vread(sj, 0, 0);
+          if (i == NQ - 1) vf[1] = vread(sj, 1 / C::DT, 1 % C::DT);
+#pragma unroll
+          for (int e = i * EX / NQ; e < (i + 1) * EX / NQ; ++e) scur[e >> 4][e & 15] = prob(scur[e >> 4][e & 15]);
+#pragma unroll
+          for (int p = 0; p < EX / 2; ++p)
+            if (2 * p + 1 >= i * EX / NQ && 2 * p + 1 < (i + 1) * EX / NQ) pack(p);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      {
+        const float first = here - (float)((j + 1) * C::BKV + 4 * g);
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          if (i + 2 < NP) vf[(i + 2) % 3] = vread(sj, (i + 2) / C::DT, (i + 2) % C::DT);
+#pragma unroll
+          for (int t = 0; t < IPW; ++t)
+            if (i == t * (NP - ND) / IPW) issue_one(j + ST - 1, (sj + ST - 1) % ST, t);
+          if (i < NP - ND) pv(vf[i % 3], pw[i / C::DT], i % C::DT);
+#pragma unroll
+          for (int e = i * 32 / NP; e < (i + 1) * 32 / NP; ++e) {
+            snext[e >> 4][e & 15] = pre(snext[e >> 4][e & 15], first, e >> 4, e & 15);
+            m = fmaxf(m, snext[e >> 4][e & 15]);
+          }
+          if (i < NPRE) {
+#pragma unroll
+            for (int e = EX + i * (32 - EX) / NPRE; e < EX + (i + 1) * (32 - EX) / NPRE; ++e)
+              scur[e >> 4][e & 15] = prob(scur[e >> 4][e & 15]);
+#pragma unroll
+            for (int p = EX / 2; p < 16; ++p)
+              if (2 * p + 1 >= EX + i * (32 - EX) / NPRE && 2 * p + 1 < EX + (i + 1) * (32 - EX) / NPRE) pack(p);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (i == (k * NP + NP - 1) / 8) add_sum(pw[k >> 1][(k & 1) * 2], pw[k >> 1][(k & 1) * 2 + 1]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mcur = max_halves(m);
+      }
+      // tile j + 2 must have landed for every wave before the next QK^T, and
+      // every wave must be done with tile j's slot before it is refilled; the
+      // last PV MFMAs, on fragments in registers, run behind the barrier
+      wait_vmcnt<(ST - 3) * IPW>();
+      __syncthreads();
+#pragma unroll
+      for (int i = NP - ND; i < NP; ++i) pv(vf[i % 3], pw[i / C::DT], i % C::DT);
+    };
+    int j = t0;
+    for (; j + 3 < tf; j += 4) {
+      tile_step(j, 0, sa, sb);
+      tile_step(j + 1, 1, sb, sa);
+      tile_step(j + 2, 2, sa, sb);
+      tile_step(j + 3, 3, sb, sa);
+    }
+    if (j < tf) tile_step(j, 0, sa, sb);
+    if (j + 1 < tf) tile_step(j + 1, 1, sb, sa);
+    if (j + 2 < tf) tile_step(j + 2, 2, sa, sb);
+  }
+
+  // Tiles that some row of the workgroup does not see whole.  Their V values that
+  // are not finite would reach the other rows too (0 * inf): they are taken out
+  // of LDS, bad[class][column] keeps the first key of each class (NaN, +inf,
+  // -inf), and the rows whose limit lies behind it get theirs at the end.
+  for (int it = tf; it < t1; ++it) {
+    const int kv0 = it * C::BKV, slot = (it - t0) % ST;
+    wait_vmcnt<0>();
+    __syncthreads();
+    for (int t = 0; t < IPW; ++t) issue_one(it + ST - 1, (slot + ST - 1) % ST, t);
+    unsigned char* vt = smem + (ST + slot) * C::TILE;
     for (int e = tid; e < C::BKV * C::RC; e += NW * 64) {
       const int R = e / C::RC, c = e - R * C::RC;
       bf16_t* p = (bf16_t*)(vt + R * C::ROW + C::pos_v(R, c) * 16);
       const u32x4 w = *(const u32x4*)p;
       uint32_t any = 0;
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        any |= ((w[x] & 0x7F80u) == 0x7F80u) | ((w[x] & 0x7F800000u) == 0x7F800000u);
-      if (any) keep_bad(bad, p, 8, c * 8, tile * C::BKV + R);
+      for (int x = 0; x < 4; ++x) any |= ((w[x] & 0x7F80u) == 0x7F80u) | ((w[x] & 0x7F800000u) == 0x7F800000u);
+      if (any) keep_bad(bad, p, 8, c * 8, kv0 + R);
     }
-  };
-  float m_run = -INFINITY, l_run = 0.f;
-  f32x16 oacc[C::DT];
-#pragma unroll
-  for (int t = 0; t < C::DT; ++t) oacc[t] = f32x16{};
-
-  if (t0 < t1)
-#pragma unroll
-    for (int s = 0; s < C::STAGES - 1; ++s) issue(t0 + s);
-
-  for (int it = t0; it < t1; ++it) {
-    const int kv0 = it * C::BKV;
-    wait_vmcnt<0>();
-    __syncthreads();
-    issue(it + C::STAGES - 1);
-    const unsigned char* slot = smem + (it % C::STAGES) * C::SLOT;
-    const bool masked = kv0 + C::BKV > lim_lo;  // some row of the workgroup does not see the whole tile
-
-    if (masked) clean_v(it);
     f32x16 s[2];
+    float m = -INFINITY;
+    const float first = here - (float)(kv0 + 4 * g);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       s[kt] = f32x16{};
 #pragma unroll
-      for (int st = 0; st < C::KS; ++st) {
-        const bf16x8 kf = *(const bf16x8*)(slot + kt * 32 * C::ROW + k_off[st]);
-        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kt], 0, 0, 0);
-      }
-    }
-    // scores in the exp2 domain (lane: key kv0 + kt*32 + 8*(e/4) + 4*g + e%4 of its own row)
-    float m = -INFINITY;
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+      for (int st = 0; st < C::KS; ++st) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(slot, kt, st), qf[st], s[kt], 0, 0, 0);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int key = kv0 + kt * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
-        float z = s[kt][e];
-        if (CAP) {
-          z = cap_out - 2.0f * cap_out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * cap_in) + 1.0f);
-        } else {
-          z *= sc;
-        }
-        if (BIAS) z -= slope * fabsf((float)(here - key));
-        if (masked && key >= lim) z = -INFINITY;
-        s[kt][e] = z;
-        m = fmaxf(m, z);
+        s[kt][e] = kv0 + kt * 32 + (e >> 2) * 8 + g * 4 + (e & 3) < lim ? pre(s[kt][e], first, kt, e) : -INFINITY;
+        m = fmaxf(m, s[kt][e]);
       }
-    m = max_halves(m);
-    if (__builtin_amdgcn_ballot_w64(m > m_run + TAU) != 0) {
-      const float m_new = fmaxf(m_run, m);
-      // nothing seen so far: O and l are zero, any finite factor will do
-      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
-      l_run *= alpha;
-#pragma unroll
-      for (int t = 0; t < C::DT; ++t) oacc[t] *= alpha;
-      m_run = m_new;
     }
-    const float mneg = m_run == -INFINITY ? 0.f : -m_run;
+    m = max_halves(m);
+    // (of a row without a visible key here, the max stays -inf whatever the cap makes of it)
+    lead(m == -INFINITY ? m : z_of_max(m));
     u32x4 pw[4];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kt][e] = __builtin_amdgcn_exp2f(s[kt][e] + mneg);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        pw[c][w] = pack_bf16x2(s[c >> 1][(c & 1) * 8 + 2 * w], s[c >> 1][(c & 1) * 8 + 2 * w + 1]);
-        l_run += __uint_as_float(pw[c][w] << 16) + __uint_as_float(pw[c][w] & 0xFFFF0000u);
+        const int e = (c & 1) * 8 + 2 * w;
+        const float x = s[c >> 1][e], y = s[c >> 1][e + 1];
+        pw[c][w] = pack_bf16x2(x == -INFINITY ? 0.f : prob(x), y == -INFINITY ? 0.f : prob(y));
+        if (w & 1) add_sum(pw[c][w - 1], pw[c][w]);
       }
-    auto vread = [&](int c, int t) {
-      typedef __attribute__((address_space(3))) s16x4* lds_p;
-      const unsigned ad = lds0 + (unsigned)((it % C::STAGES) * C::SLOT + v_off[t] + c * 16 * C::ROW);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(size_t)ad);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(size_t)(ad + 8 * C::ROW));
-      const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
-      return u32x4{l2[0], l2[1], h2[0], h2[1]};
-    };
-    if (masked) __syncthreads();  // the tile's V has been cleaned
+    __syncthreads();  // V has been cleaned
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int t = 0; t < C::DT; ++t)
-        oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vread(c, t)),
-                                                          __builtin_bit_cast(bf16x8, pw[c]), oacc[t], 0, 0, 0);
+      for (int t = 0; t < C::DT; ++t) pv(vread(slot, c, t), pw[c], t);
   }
   wait_vmcnt<0>();
   __syncthreads();
-  if (lim_lo < nkv_all * C::BKV)
+  const float l_tot = sum_halves(C::FOLD ? (g == C::LG ? oacc[C::LT][C::LE] : 0.f) : lacc[0]);
+  if (tf < t1)
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
 #pragma unroll
@@ -241,7 +387,6 @@ __global__ __launch_bounds__(NW * 64) void doc_attn_bf16_kernel(DocAttnArgs a) {
         if (d < DH) oacc[t][e] = add_bad(oacc[t][e], bad, d, lim);
       }
 
-  const float l_tot = sum_halves(l_run);
   const bool live = r0 + r32 < rows;
   if (a.split > 1) {
     if (!live) return;
@@ -315,7 +460,7 @@ __global__ __launch_bounds__(256) void doc_attn_merge_kernel(DocAttnArgs a) {
 
 template <int DH>
 static hipError_t launch_dh(const DocAttnArgs& a, hipStream_t st) {
-  constexpr int NW = 4;
+  constexpr int NW = 8;
   const long nqb = ((long)a.max_q * a.G + NW * 32 - 1) / (NW * 32);
   const dim3 grid((unsigned)(nqb * a.Hk), a.docs, a.split), block(NW * 64);
   const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
