@@ -63,6 +63,50 @@ __device__ __forceinline__ s16x4 read_tr(const lds_byte* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p);
 }
 
+// A row's scores, raw -> z (the exponent in the exp2 domain) -> probability.  The
+// scale and the cap keep the order of scores, so that they can wait for the
+// exponential, after the row max; the bias cannot.
+template <bool CAP, bool BIAS>
+struct DocScore {
+  float sc, cap_in, cap_out, slope, here;
+  __device__ __forceinline__ DocScore(const DocAttnArgs& a, int h, int place) {
+    sc = a.scale * LOG2E;
+    cap_in = CAP ? 2.0f * sc / a.cap : 0.f;
+    cap_out = CAP ? a.cap * LOG2E : 0.f;
+    slope = BIAS ? a.slopes[h] * LOG2E : 0.f;
+    here = (float)place;  // the key at the row's own place
+  }
+  // cap tanh(s scale / cap) = cap - 2 cap / (exp(2 s scale / cap) + 1), plus `more`, in the exp2 domain
+  __device__ __forceinline__ float capped(float s, float more) const {
+    return fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * cap_in) + 1.0f), cap_out + more);
+  }
+  // before the max; the key is `first - off` places before the row's own
+  __device__ __forceinline__ float pre(float s, float first, int off) const {
+    if (!BIAS) return s;
+    return fmaf(-slope, fabsf(first - (float)off), CAP ? capped(s, 0.f) : s * sc);
+  }
+  __device__ __forceinline__ float z_of_max(float m) const { return BIAS ? m : CAP ? capped(m, 0.f) : m * sc; }
+  __device__ __forceinline__ float prob(float s, float mneg) const {
+    return __builtin_amdgcn_exp2f(BIAS ? s + mneg : CAP ? capped(s, mneg) : fmaf(s, sc, mneg));
+  }
+};
+
+// Values of a V tile (n_rows rows in LDS from vt, key kv0 on) that are not
+// finite are noted in bad and become 0; nt threads share the work.
+template <int DH>
+__device__ __forceinline__ void clean_v(int (&bad)[3][DH], unsigned char* vt, int kv0, int t, int nt) {
+  using C = DocCfg<DH>;
+  for (int e = t; e < C::BKV * C::RC; e += nt) {
+    const int R = e / C::RC, c = e - R * C::RC;
+    bf16_t* p = (bf16_t*)(vt + R * C::ROW + C::pos_v(R, c) * 16);
+    const u32x4 w = *(const u32x4*)p;
+    uint32_t any = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) any |= ((w[x] & 0x7F80u) == 0x7F80u) | ((w[x] & 0x7F800000u) == 0x7F800000u);
+    if (any) keep_bad(bad, p, 8, c * 8, kv0 + R);
+  }
+}
+
 template <int DH, int NW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a) {
   using C = DocCfg<DH>;
@@ -116,19 +160,28 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
   // chunk of head_dim 72's rows is no lane's: it keeps what is written below.
   // Past the last tile, and for spare instructions, the copy goes to the spare
   // line, so that every wave counts the same.
-  auto issue_one = [&](int tile, int slot, int t) {
+  const int kv_last = (t1 - 1) * C::BKV;  // (some of its rows may lie past the end)
+  unsigned off[IPW], off_last[IPW];
+  bool copies[IPW];
+#pragma unroll
+  for (int t = 0; t < IPW; ++t) {
     const int i = wave + NW * t;  // wave-uniform
     const bool real = !SPARE || i < 2 * C::DMA, isv = real && i >= C::DMA;
-    const int kv0 = min(tile, t1 - 1) * C::BKV;
     const int byte = (isv ? i - C::DMA : real ? i : 0) * 1024 + lane * 16;
-    const int R = byte / C::ROW, pos = (byte % C::ROW) >> 4;
-    const int c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
-    const long rs = isv ? a.v_row : a.k_row;
-    const bf16_t* base = (isv ? vp : kp) + kv0 * rs;
-    const unsigned off = (unsigned)min(R, doc.nk - 1 - kv0) * (unsigned)(rs * 2) + c * 16;
+    const int R = byte / C::ROW, pos = (byte % C::ROW) >> 4, c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
+    const unsigned rs = (unsigned)(isv ? a.v_row : a.k_row) * 2;
+    off[t] = R * rs + c * 16;
+    off_last[t] = min(R, doc.nk - 1 - kv_last) * rs + c * 16;
+    copies[t] = C::CPR == C::RC || c < C::RC;
+  }
+  auto issue_one = [&](int tile, int slot, int t) {
+    const int i = wave + NW * t;
+    const bool real = !SPARE || i < 2 * C::DMA, isv = real && i >= C::DMA;
+    const int tl = min(tile, t1 - 1);
+    const bf16_t* base = isv ? vp + (long)(tl * C::BKV) * a.v_row : kp + (long)(tl * C::BKV) * a.k_row;
     const unsigned dst = real && tile < t1 ? lds0 + (isv ? (ST + slot) * C::TILE + (i - C::DMA) * 1024 : slot * C::TILE + i * 1024)
                                            : lds0 + 2 * ST * C::TILE;
-    if (C::CPR == C::RC || c < C::RC) dma_16s(base, off, dst);
+    if (copies[t]) dma_16s(base, tl == t1 - 1 ? off_last[t] : off[t], dst);
   };
   for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
   if (C::FOLD) {
@@ -162,32 +215,10 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     return u32x4{lo[0], lo[1], hi[0], hi[1]};
   };
 
-  // A score goes raw -> z (the exponent in the exp2 domain).  The scale and the
-  // cap keep the order of scores, so that they can wait for the exponential,
-  // after the row max; the bias cannot.
-  const float sc = a.scale * LOG2E;
-  const float cap_in = CAP ? 2.0f * sc / a.cap : 0.f, cap_out = CAP ? a.cap * LOG2E : 0.f;
-  const float slope = BIAS ? a.slopes[h] * LOG2E : 0.f;
-  const float here = (float)(qi + doc.nk - doc.nq);
-  auto capped = [&](float s) {  // cap tanh(s scale / cap), in the exp2 domain
-    return fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * cap_in) + 1.0f), cap_out);
-  };
-  // before the max: element e of half kt of a tile whose first key, less 4 g, is
-  // `first` keys behind the row's own place
-  auto pre = [&](float s, float first, int kt, int e) {
-    if (!BIAS) return s;
-    const float z = CAP ? capped(s) : s * sc;
-    return fmaf(-slope, fabsf(first - (float)(kt * 32 + (e >> 2) * 8 + (e & 3))), z);
-  };
-  auto z_of_max = [&](float m) { return BIAS ? m : CAP ? capped(m) : m * sc; };
+  const DocScore<CAP, BIAS> score(a, h, qi + doc.nk - doc.nq);
+  auto pre = [&](float x, float first, int kt, int e) { return score.pre(x, first, kt * 32 + (e >> 2) * 8 + (e & 3)); };
   float m_run = -INFINITY, mneg = 0.f;  // mneg = -m_run, 0 while nothing has been seen
-  auto prob = [&](float s) {
-    if (BIAS) return __builtin_amdgcn_exp2f(s + mneg);
-    if (CAP)
-      return __builtin_amdgcn_exp2f(
-          fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * cap_in) + 1.0f), cap_out + mneg));
-    return __builtin_amdgcn_exp2f(fmaf(s, sc, mneg));
-  };
+  auto prob = [&](float x) { return score.prob(x, mneg); };
   const float TAU = 64.0f;
   // Row sums of the bf16 probabilities (the values the PV product multiplies) on
   // the matrix pipe: a 4x4x4 MFMA with ones adds the four of a lane's operand.
@@ -234,7 +265,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     }
     float mcur = -INFINITY;  // row max of the current tile (what pre() gives), both halves
     {
-      const float first = here - (float)(t0 * C::BKV + 4 * g);
+      const float first = score.here - (float)(t0 * C::BKV + 4 * g);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -249,7 +280,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     // max of tile j + 1 and the DMA of tile j + 3.  (The last tile's QK^T reads
     // the slot behind it: computed, and not used.)
     auto tile_step = [&](const int j, const int sj, f32x16 (&scur)[2], f32x16 (&snext)[2]) __attribute__((always_inline)) {
-      lead(z_of_max(mcur));
+      lead(score.z_of_max(mcur));
       constexpr int EX = C::FOLD ? 16 : 24;  // exponentials beside QK^T; the rest beside the first PV MFMAs
       constexpr int NP = 4 * C::DT, NPRE = EX / 8 * C::DT, ND = 3, NQ = 2 * C::KS;
       u32x4 pw[4], vf[3];
@@ -274,7 +305,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
         }
       }
       {
-        const float first = here - (float)((j + 1) * C::BKV + 4 * g);
+        const float first = score.here - (float)((j + 1) * C::BKV + 4 * g);
         float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -332,19 +363,10 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     wait_vmcnt<0>();
     __syncthreads();
     for (int t = 0; t < IPW; ++t) issue_one(it + ST - 1, (slot + ST - 1) % ST, t);
-    unsigned char* vt = smem + (ST + slot) * C::TILE;
-    for (int e = tid; e < C::BKV * C::RC; e += NW * 64) {
-      const int R = e / C::RC, c = e - R * C::RC;
-      bf16_t* p = (bf16_t*)(vt + R * C::ROW + C::pos_v(R, c) * 16);
-      const u32x4 w = *(const u32x4*)p;
-      uint32_t any = 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) any |= ((w[x] & 0x7F80u) == 0x7F80u) | ((w[x] & 0x7F800000u) == 0x7F800000u);
-      if (any) keep_bad(bad, p, 8, c * 8, kv0 + R);
-    }
+    clean_v<DH>(bad, smem + (ST + slot) * C::TILE, kv0, tid, NW * 64);
     f32x16 s[2];
     float m = -INFINITY;
-    const float first = here - (float)(kv0 + 4 * g);
+    const float first = score.here - (float)(kv0 + 4 * g);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       s[kt] = f32x16{};
@@ -358,7 +380,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     }
     m = max_halves(m);
     // (of a row without a visible key here, the max stays -inf whatever the cap makes of it)
-    lead(m == -INFINITY ? m : z_of_max(m));
+    lead(m == -INFINITY ? m : score.z_of_max(m));
     u32x4 pw[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -425,12 +447,207 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     }
 }
 
+// Few rows (at most 32 of a document and key head: single tokens over a cache):
+// bound by the keys' and values' bytes.  The four waves of a workgroup take the
+// 64-key tiles of its range in turn, each with a ring of its own (one K and one V
+// tile, refilled as soon as it is used up) and a softmax state of its own, and no
+// barrier until the four states are merged through LDS.
+template <int DH, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
+  using C = DocCfg<DH>;
+  constexpr int NW = 4, OS = DH + 4;
+  constexpr int RING = 2 * C::TILE + 256;  // of one wave (+ what transposed reads of head_dim 72 touch past V)
+  static_assert(NW * RING >= NW * 32 * OS * 4, "the states are merged where the rings were");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * RING];
+  __shared__ float ml[NW][2][32];
+  __shared__ int bad[3][DH];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, r32 = lane & 31;
+  const Doc doc = load_doc(a, blockIdx.y);
+  const int rows = doc.nq * a.G, hk = blockIdx.x, part = blockIdx.z;
+  if (rows == 0) return;
+  const int row = min(r32, rows - 1);
+  const int qi = row / a.G, h = hk * a.G + row % a.G;
+  const int lim = row_limit(a, doc, qi), lim_lo = row_limit(a, doc, 0), lim_hi = row_limit(a, doc, doc.nq - 1);
+  const int nkv_all = (lim_hi + C::BKV - 1) / C::BKV;
+  const int t0 = (int)((long)nkv_all * part / a.split), t1 = (int)((long)nkv_all * (part + 1) / a.split);
+
+  const bf16_t* __restrict__ kp = (const bf16_t*)a.k + (long)doc.k0 * a.k_row + hk * a.k_head;
+  const bf16_t* __restrict__ vp = (const bf16_t*)a.v + (long)doc.k0 * a.v_row + hk * a.v_head;
+  const bf16_t* __restrict__ qp = (const bf16_t*)a.q + (long)(doc.q0 + qi) * a.q_row + h * a.q_head;
+  unsigned char* ring = smem + wave * RING;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(ring));
+
+  auto issue = [&](int tile, bool isv) {
+    const int kv0 = tile * C::BKV;
+    const long rs = isv ? a.v_row : a.k_row;
+    const bf16_t* base = (isv ? vp : kp) + (long)kv0 * rs;
+#pragma unroll
+    for (int i = 0; i < C::DMA; ++i) {
+      const int byte = i * 1024 + lane * 16, R = byte / C::ROW, pos = (byte % C::ROW) >> 4;
+      const int c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
+      const unsigned off = (unsigned)min(R, doc.nk - 1 - kv0) * (unsigned)(rs * 2) + c * 16;
+      if (C::CPR == C::RC || c < C::RC) dma_16s(base, off, lds0 + (isv ? C::TILE : 0) + i * 1024);
+    }
+  };
+  if (t0 + wave < t1) {
+    issue(t0 + wave, false);
+    issue(t0 + wave, true);
+  }
+  bf16x8 qf[C::KS];
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s)
+    qf[s] = s * 16 + g * 8 < DH ? *(const bf16x8*)(qp + s * 16 + g * 8) : bf16x8{};
+  for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
+  if (C::CPR > C::RC) {
+    ((uint32_t*)(ring + 2 * C::TILE))[lane] = 0;
+    for (int e = lane; e < 2 * C::BKV * 4; e += 64) {
+      const int R = (e >> 2) & (C::BKV - 1), isv = e >> 8;
+      ((uint32_t*)(ring + isv * C::TILE + R * C::ROW + (isv ? C::pos_v(R, C::RC) : C::pos_k(R, C::RC)) * 16))[e & 3] = 0;
+    }
+  }
+  __syncthreads();
+
+  const lds_byte* k_at[C::KS];
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s) k_at[s] = (const lds_byte*)ring + r32 * C::ROW + (C::pos_k(r32, 2 * s + g) << 4);
+  const lds_byte* v_at[C::DT];
+  {
+    const int R = 4 * g + ((lane & 15) >> 2), half = (lane >> 4) & 1;
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t)
+      v_at[t] = (const lds_byte*)ring + C::TILE + R * C::ROW +
+                (C::pos_v(R, t * 4 + half * 2 + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
+  }
+  const DocScore<CAP, BIAS> score(a, h, qi + doc.nk - doc.nq);
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 oacc[C::DT];
+#pragma unroll
+  for (int t = 0; t < C::DT; ++t) oacc[t] = f32x16{};
+  // Q and the slope are here before the loop, whose waits count DMA alone
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s) asm volatile("" : "+v"(qf[s]));
+  if (BIAS) asm volatile("" : : "v"(score.slope));
+  wait_vmcnt<0>();
+
+  for (int it = t0 + wave; it < t1; it += NW) {
+    const int kv0 = it * C::BKV;
+    const bool more = it + NW < t1, masked = kv0 + C::BKV > lim_lo;
+    if (it > t0 + wave) wait_vmcnt<C::DMA>();  // this tile's K (its V, issued behind it, may still be under way)
+    f32x16 s[2];
+    float m = -INFINITY;
+    const float first = score.here - (float)(kv0 + 4 * g);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      s[kt] = f32x16{};
+#pragma unroll
+      for (int st = 0; st < C::KS; ++st)
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            *(const __attribute__((address_space(3))) bf16x8*)(k_at[st] + kt * 32 * C::ROW), qf[st], s[kt], 0, 0, 0);
+    }
+    // the products have read K: its slot takes the next tile's
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) issue(it + NW, false);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int off = kt * 32 + (e >> 2) * 8 + (e & 3);
+        s[kt][e] = kv0 + off + g * 4 < lim ? score.pre(s[kt][e], first, off) : -INFINITY;
+        m = fmaxf(m, s[kt][e]);
+      }
+    m = max_halves(m);
+    m = m == -INFINITY ? m : score.z_of_max(m);
+    const float m_new = fmaxf(m_run, m), mneg = m_new == -INFINITY ? 0.f : -m_new;
+    const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+    l_run *= alpha;
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t) oacc[t] *= alpha;
+    m_run = m_new;
+    u32x4 pw[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int e = (c & 1) * 8 + 2 * w;
+        const float x = s[c >> 1][e], y = s[c >> 1][e + 1];
+        pw[c][w] = pack_bf16x2(x == -INFINITY ? 0.f : score.prob(x, mneg), y == -INFINITY ? 0.f : score.prob(y, mneg));
+        l_run += __uint_as_float(pw[c][w] << 16) + __uint_as_float(pw[c][w] & 0xFFFF0000u);
+      }
+    if (more) wait_vmcnt<C::DMA>();  // this tile's V (the next K may be under way)
+    else wait_vmcnt<0>();
+    if (masked) {
+      clean_v<DH>(bad, ring + C::TILE, kv0, lane, 64);
+      wave_lds_fence();
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int t = 0; t < C::DT; ++t) {
+        const lds_byte* p = v_at[t] + c * 16 * C::ROW;
+        const u32x2 lo = __builtin_bit_cast(u32x2, read_tr(p)), hi = __builtin_bit_cast(u32x2, read_tr(p + 8 * C::ROW));
+        oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]}),
+                                                          __builtin_bit_cast(bf16x8, pw[c]), oacc[t], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) issue(it + NW, true);
+  }
+
+  __syncthreads();  // every ring has been read
+  float* os = (float*)smem + wave * 32 * OS;
+  l_run = sum_halves(l_run);
+  if (r32 < rows) {
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const int d = t * 32 + jj * 8 + g * 4;
+        if (d < DH)
+          *(f32x4*)(os + r32 * OS + d) = f32x4{oacc[t][jj * 4 + 0], oacc[t][jj * 4 + 1], oacc[t][jj * 4 + 2], oacc[t][jj * 4 + 3]};
+      }
+    if (g == 0) ml[wave][0][r32] = m_run, ml[wave][1][r32] = l_run;
+  }
+  __syncthreads();
+  constexpr int G4 = DH / 4;
+  for (int i = tid; i < rows * G4; i += NW * 64) {
+    const int r = i / G4, d = (i - r * G4) * 4, qr = r / a.G, hr = hk * a.G + r % a.G;
+    float mx = ml[0][0][r];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mx = fmaxf(mx, ml[w][0][r]);
+    const float mr = mx == -INFINITY ? 0.f : mx;
+    float den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[w][0][r] - mr);
+      den += f * ml[w][1][r];
+      num += f * *(const f32x4*)((const float*)smem + (w * 32 + r) * OS + d);
+    }
+    const int lim_r = row_limit(a, doc, qr);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) num[x] = add_bad(num[x], bad, d + x, lim_r);
+    if (a.split > 1) {
+      float* pr = a.part + ((long)part * a.q_rows * a.H + (long)(doc.q0 + qr) * a.H + hr) * (DH + 4);
+      *(f32x4*)(pr + d) = num;
+      if (d == 0) *(f32x2*)(pr + DH) = f32x2{mx, den};
+    } else {
+      const float inv = den == 0.f ? 0.f : 1.0f / den;
+      bf16_t* op = (bf16_t*)a.o + (long)(doc.q0 + qr) * a.o_row + hr * a.o_head + d;
+      *(u32x2*)op = u32x2{pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv)};
+    }
+  }
+}
+
 // Joins the key ranges of a split call: with m = max_s m_s and f_s = 2^(m_s - m),
-// O = sum_s f_s O_s / sum_s f_s l_s, ranges in order.  One thread takes four
-// columns of one (query, head).
+// O = sum_s f_s O_s / sum_s f_s l_s, ranges in order, eight loading at a time.
+// One thread takes four columns of one (query, head).
 template <int DH, typename T>
 __global__ __launch_bounds__(256) void doc_attn_merge_kernel(DocAttnArgs a) {
-  constexpr int G4 = DH / 4;
+  constexpr int G4 = DH / 4, U = 8;
   const Doc doc = load_doc(a, blockIdx.y);
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
   const long rh = i / G4;
@@ -438,17 +655,32 @@ __global__ __launch_bounds__(256) void doc_attn_merge_kernel(DocAttnArgs a) {
   const int d = (int)(i - rh * G4) * 4, qi = (int)(rh / a.H), h = (int)(rh - (long)qi * a.H);
   const float* p = a.part + ((long)(doc.q0 + qi) * a.H + h) * (DH + 4);
   const long stride = (long)a.q_rows * a.H * (DH + 4);
-  float m = -INFINITY;
-  for (int s = 0; s < a.split; ++s) m = fmaxf(m, p[s * stride + DH]);
-  const float mr = m == -INFINITY ? 0.f : m;
-  float den = 0.f;
+  float m = -INFINITY, den = 0.f;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.split; ++s) {
-    const f32x2 ml = *(const f32x2*)(p + s * stride + DH);
-    const float f = __builtin_amdgcn_exp2f(ml[0] - mr);
-    // an empty range has m = -inf and zeros
-    den += f * ml[1];
-    num += f * *(const f32x4*)(p + s * stride + d);
+  for (int s0 = 0; s0 < a.split; s0 += U) {
+    f32x2 ml[U];
+    f32x4 o[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* ps = p + min(s0 + u, a.split - 1) * stride;
+      ml[u] = *(const f32x2*)(ps + DH);
+      o[u] = *(const f32x4*)(ps + d);
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u][0]);
+    const float mr = top == -INFINITY ? 0.f : top;  // an empty range has m = -inf and zeros
+    const float keep = __builtin_amdgcn_exp2f(m - mr);
+    den *= keep;
+    num *= keep;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s0 + u < a.split) {
+        const float f = __builtin_amdgcn_exp2f(ml[u][0] - mr);
+        den += f * ml[u][1];
+        num += f * o[u];
+      }
+    m = top;
   }
   const float inv = den == 0.f ? 0.f : 1.0f / den;
   T* op = (T*)a.o + (long)(doc.q0 + qi) * a.o_row + h * a.o_head + d;
@@ -458,24 +690,31 @@ __global__ __launch_bounds__(256) void doc_attn_merge_kernel(DocAttnArgs a) {
     *(f32x4*)op = num * inv;
 }
 
+template <int DH, bool CAP, bool BIAS>
+static void launch_score(const DocAttnArgs& a, const DocAttnPlan& p, hipStream_t st) {
+  if (p.kernel == DOC_FEW) {
+    hipLaunchKernelGGL((doc_attn_few_kernel<DH, CAP, BIAS>), dim3(a.Hk, a.docs, a.split), dim3(256), 0, st, a);
+  } else {
+    const long nqb = ((long)a.max_q * a.G + 255) / 256;
+    hipLaunchKernelGGL((doc_attn_bf16_kernel<DH, 8, CAP, BIAS>), dim3((unsigned)(nqb * a.Hk), a.docs, a.split), dim3(512), 0, st, a);
+  }
+}
+
 template <int DH>
-static hipError_t launch_dh(const DocAttnArgs& a, hipStream_t st) {
-  constexpr int NW = 8;
-  const long nqb = ((long)a.max_q * a.G + NW * 32 - 1) / (NW * 32);
-  const dim3 grid((unsigned)(nqb * a.Hk), a.docs, a.split), block(NW * 64);
+static hipError_t launch_dh(const DocAttnArgs& a, const DocAttnPlan& p, hipStream_t st) {
   const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
-  if (cap && bias) hipLaunchKernelGGL((doc_attn_bf16_kernel<DH, NW, true, true>), grid, block, 0, st, a);
-  else if (cap) hipLaunchKernelGGL((doc_attn_bf16_kernel<DH, NW, true, false>), grid, block, 0, st, a);
-  else if (bias) hipLaunchKernelGGL((doc_attn_bf16_kernel<DH, NW, false, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((doc_attn_bf16_kernel<DH, NW, false, false>), grid, block, 0, st, a);
+  if (cap && bias) launch_score<DH, true, true>(a, p, st);
+  else if (cap) launch_score<DH, true, false>(a, p, st);
+  else if (bias) launch_score<DH, false, true>(a, p, st);
+  else launch_score<DH, false, false>(a, p, st);
   return hipGetLastError();
 }
 
 hipError_t launch_doc_attn_bf16(const DocAttnArgs& a, const DocAttnPlan& p, int head_dim, hipStream_t st) {
   switch (head_dim) {
-    case 64: return launch_dh<64>(a, st);
-    case 72: return launch_dh<72>(a, st);
-    case 128: return launch_dh<128>(a, st);
+    case 64: return launch_dh<64>(a, p, st);
+    case 72: return launch_dh<72>(a, p, st);
+    case 128: return launch_dh<128>(a, p, st);
     default: return hipErrorInvalidValue;
   }
 }
@@ -497,16 +736,20 @@ hipError_t launch_doc_attn_merge(const DocAttnArgs& a, int head_dim, int dtype, 
   return hipGetLastError();
 }
 
-// A grid of fewer than 256 workgroups leaves compute units idle: the keys are
-// divided until there are about two workgroups for each, with at least four
-// tiles per range.
+// At most 32 rows of a document and key head (bf16) go to the kernel of few rows.
+// A grid that leaves compute units idle divides the keys of its items into
+// ranges, of four tiles (256 keys; fp32: 128) at least, until there is a
+// workgroup for each unit (fp32, and few rows of 64: two).
 DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype) {
   DocAttnPlan p{DOC_ROWS, 1};
-  const long bm = 128;
-  const long per_doc = ((long)a.max_q * a.G + bm - 1) / bm;
+  const long rows = (long)a.max_q * a.G;
+  if (dtype == 1 && rows <= 32) p.kernel = DOC_FEW;
+  const long bm = p.kernel == DOC_FEW ? 32 : dtype == 1 ? 256 : 16;
+  const long per_doc = (rows + bm - 1) / bm;
   const long items = a.Hk * std::max(1L, std::min(a.docs * per_doc, (long)a.q_rows * a.G / bm + a.docs));
-  const long tiles = ((long)a.max_k + 63) / 64;
-  if (items < 256) p.split = (int)std::max(1L, std::min({512 / items, tiles / 4, 32L}));
+  const long tiles = (long)a.max_k / (dtype == 1 ? 256 : 128);
+  const long want = dtype == 1 && (p.kernel == DOC_ROWS || head_dim != 64) ? 256 : 512;
+  if (items * 2 <= want) p.split = (int)std::max(1L, std::min({want / items, tiles, 32L}));
   return p;
 }
 

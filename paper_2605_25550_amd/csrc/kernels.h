@@ -144,7 +144,7 @@ struct DocAttnPlan {
   int kernel;  // DOC_*
   int split;
 };
-enum { DOC_ROWS = 0, DOC_SPLIT = 1 };  // waves own rows / waves of a workgroup share 32 rows and divide the keys
+enum { DOC_ROWS = 0, DOC_FEW = 1 };  // waves own rows / the waves of a workgroup share 32 rows and divide the keys
 DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype);
 
 // ------------------------------------------------------------------ 8-bit products, block scales of 128
