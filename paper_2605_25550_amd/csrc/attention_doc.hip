@@ -91,19 +91,28 @@ struct DocScore {
   }
 };
 
-// Values of a V tile (n_rows rows in LDS from vt, key kv0 on) that are not
-// finite are noted in bad and become 0; nt threads share the work.
-template <int DH>
-__device__ __forceinline__ void clean_v(int (&bad)[3][DH], unsigned char* vt, int kv0, int t, int nt) {
+// Values of a V tile (in LDS from vt, key kv0 on) that are not finite are noted
+// in bad and become 0; NT threads share the work, all their reads in flight.
+template <int DH, int NT>
+__device__ __forceinline__ void clean_v(int (&bad)[3][DH], unsigned char* vt, int kv0, int t) {
   using C = DocCfg<DH>;
-  for (int e = t; e < C::BKV * C::RC; e += nt) {
-    const int R = e / C::RC, c = e - R * C::RC;
-    bf16_t* p = (bf16_t*)(vt + R * C::ROW + C::pos_v(R, c) * 16);
-    const u32x4 w = *(const u32x4*)p;
+  constexpr int N = C::BKV * C::RC, PER = (N + NT - 1) / NT;
+  auto at = [&](int i) {
+    const int e = min(t + i * NT, N - 1), R = e / C::RC, c = e - R * C::RC;
+    return (bf16_t*)(vt + R * C::ROW + C::pos_v(R, c) * 16);
+  };
+  uint32_t odd = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const u32x4 w = *(const u32x4*)at(i);
     uint32_t any = 0;
 #pragma unroll
     for (int x = 0; x < 4; ++x) any |= ((w[x] & 0x7F80u) == 0x7F80u) | ((w[x] & 0x7F800000u) == 0x7F800000u);
-    if (any) keep_bad(bad, p, 8, c * 8, kv0 + R);
+    odd |= any << i;
+  }
+  for (; odd; odd &= odd - 1) {
+    const int i = __builtin_ctz(odd), e = min(t + i * NT, N - 1), R = e / C::RC;
+    keep_bad(bad, at(i), 8, (e - R * C::RC) * 8, kv0 + R);
   }
 }
 
@@ -363,7 +372,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     wait_vmcnt<0>();
     __syncthreads();
     for (int t = 0; t < IPW; ++t) issue_one(it + ST - 1, (slot + ST - 1) % ST, t);
-    clean_v<DH>(bad, smem + (ST + slot) * C::TILE, kv0, tid, NW * 64);
+    clean_v<DH, NW * 64>(bad, smem + (ST + slot) * C::TILE, kv0, tid);
     f32x16 s[2];
     float m = -INFINITY;
     const float first = score.here - (float)(kv0 + 4 * g);
@@ -447,9 +456,9 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     }
 }
 
-// Few rows (at most 32 of a document and key head: single tokens over a cache):
-// bound by the keys' and values' bytes.  The four waves of a workgroup take the
-// 64-key tiles of its range in turn, each with a ring of its own (one K and one V
+// Few rows (single tokens over a cache, bound by the keys' and values' bytes, and
+// small grids, bound by the chain of tiles): a workgroup owns 32 rows, and its four
+// waves take the 64-key tiles of its range in turn, each with a ring of its own (one K and one V
 // tile, refilled as soon as it is used up) and a softmax state of its own, and no
 // barrier until the four states are merged through LDS.
 template <int DH, bool CAP, bool BIAS>
@@ -466,11 +475,13 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r32 = lane & 31;
   const Doc doc = load_doc(a, blockIdx.y);
-  const int rows = doc.nq * a.G, hk = blockIdx.x, part = blockIdx.z;
-  if (rows == 0) return;
-  const int row = min(r32, rows - 1);
+  const int all_rows = doc.nq * a.G, nrb = (all_rows + 31) / 32, items = nrb * a.Hk, part = blockIdx.z;
+  if ((int)blockIdx.x >= items) return;
+  const int item = xcd_remap(blockIdx.x, items), hk = item / nrb, rb0 = item % nrb * 32;
+  const int rows = min(32, all_rows - rb0);  // of this workgroup, from rb0 on
+  const int row = rb0 + min(r32, rows - 1);
   const int qi = row / a.G, h = hk * a.G + row % a.G;
-  const int lim = row_limit(a, doc, qi), lim_lo = row_limit(a, doc, 0), lim_hi = row_limit(a, doc, doc.nq - 1);
+  const int lim = row_limit(a, doc, qi), lim_lo = row_limit(a, doc, rb0 / a.G), lim_hi = row_limit(a, doc, (rb0 + rows - 1) / a.G);
   const int nkv_all = (lim_hi + C::BKV - 1) / C::BKV;
   const int t0 = (int)((long)nkv_all * part / a.split), t1 = (int)((long)nkv_all * (part + 1) / a.split);
 
@@ -580,7 +591,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     if (more) wait_vmcnt<C::DMA>();  // this tile's V (the next K may be under way)
     else wait_vmcnt<0>();
     if (masked) {
-      clean_v<DH>(bad, ring + C::TILE, kv0, lane, 64);
+      clean_v<DH, 64>(bad, ring + C::TILE, kv0, lane);
       wave_lds_fence();
     }
 #pragma unroll
@@ -614,7 +625,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   __syncthreads();
   constexpr int G4 = DH / 4;
   for (int i = tid; i < rows * G4; i += NW * 64) {
-    const int r = i / G4, d = (i - r * G4) * 4, qr = r / a.G, hr = hk * a.G + r % a.G;
+    const int r = i / G4, d = (i - r * G4) * 4, qr = (rb0 + r) / a.G, hr = hk * a.G + (rb0 + r) % a.G;
     float mx = ml[0][0][r];
 #pragma unroll
     for (int w = 1; w < NW; ++w) mx = fmaxf(mx, ml[w][0][r]);
@@ -693,7 +704,7 @@ __global__ __launch_bounds__(256) void doc_attn_merge_kernel(DocAttnArgs a) {
 template <int DH, bool CAP, bool BIAS>
 static void launch_score(const DocAttnArgs& a, const DocAttnPlan& p, hipStream_t st) {
   if (p.kernel == DOC_FEW) {
-    hipLaunchKernelGGL((doc_attn_few_kernel<DH, CAP, BIAS>), dim3(a.Hk, a.docs, a.split), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((doc_attn_few_kernel<DH, CAP, BIAS>), dim3((unsigned)(((long)a.max_q * a.G + 31) / 32 * a.Hk), a.docs, a.split), dim3(256), 0, st, a);
   } else {
     const long nqb = ((long)a.max_q * a.G + 255) / 256;
     hipLaunchKernelGGL((doc_attn_bf16_kernel<DH, 8, CAP, BIAS>), dim3((unsigned)(nqb * a.Hk), a.docs, a.split), dim3(512), 0, st, a);
@@ -736,20 +747,25 @@ hipError_t launch_doc_attn_merge(const DocAttnArgs& a, int head_dim, int dtype, 
   return hipGetLastError();
 }
 
-// At most 32 rows of a document and key head (bf16) go to the kernel of few rows.
+// bf16: up to 32 rows of a document and key head, and grids that its 32-row
+// workgroups do not fill (one for each CU; two of head_dim 64), go to the kernel
+// of few rows (one document of 256 tokens, 16 heads of 72: ROWFEW us against 10.6).
 // A grid that leaves compute units idle divides the keys of its items into
 // ranges, of four tiles (256 keys; fp32: 128) at least, until there is a
-// workgroup for each unit (fp32, and few rows of 64: two).
+// workgroup for each unit (fp32, and few rows of 64: two).  More ranges cost more
+// in the merge than they gain (single tokens over 4 caches 17.8 us, 22 with
+// twice as many).
 DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype) {
   DocAttnPlan p{DOC_ROWS, 1};
   const long rows = (long)a.max_q * a.G;
-  if (dtype == 1 && rows <= 32) p.kernel = DOC_FEW;
-  const long bm = p.kernel == DOC_FEW ? 32 : dtype == 1 ? 256 : 16;
-  const long per_doc = (rows + bm - 1) / bm;
-  const long items = a.Hk * std::max(1L, std::min(a.docs * per_doc, (long)a.q_rows * a.G / bm + a.docs));
-  const long tiles = (long)a.max_k / (dtype == 1 ? 256 : 128);
-  const long want = dtype == 1 && (p.kernel == DOC_ROWS || head_dim != 64) ? 256 : 512;
-  if (items * 2 <= want) p.split = (int)std::max(1L, std::min({want / items, tiles, 32L}));
+  auto items = [&](long bm) {
+    return a.Hk * std::max(1L, std::min(a.docs * ((rows + bm - 1) / bm), (long)a.q_rows * a.G / bm + a.docs));
+  };
+  const long fill = dtype == 1 && head_dim != 64 ? 256 : 512;
+  if (dtype == 1 && (rows <= 32 || items(32) <= fill)) p.kernel = DOC_FEW;
+  const long n = items(p.kernel == DOC_FEW ? 32 : dtype == 1 ? 256 : 16);
+  const long want = dtype == 1 && p.kernel == DOC_ROWS ? 256 : fill;
+  if (n * 2 <= want) p.split = (int)std::max(1L, std::min({want / n, (long)a.max_k / (dtype == 1 ? 256 : 128), 32L}));
   return p;
 }
 

@@ -1,5 +1,6 @@
 // Masked attention over documents, fp32 (ditmi.h: dit_attention): fp32 products
-// on the matrix cores (v_mfma_f32_16x16x4_f32), fp32 exp, tanh and sums.
+// on the matrix cores (v_mfma_f32_16x16x4_f32), fp32 exponentials (the hardware's
+// 2^x, within an ulp), tanh and sums.
 //
 // A workgroup of four waves owns 16 QT rows (query, head of the group that
 // shares keys) of one document.  The waves divide the keys of the workgroup's
@@ -57,7 +58,7 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
     const int row = min(qb * BM + 16 * t + r16, rows - 1), qi = row / a.G, h = hk * a.G + row % a.G;
     lim[t] = row_limit(a, doc, qi);
     here[t] = qi + doc.nk - doc.nq;
-    slope[t] = BIAS ? a.slopes[h] : 0.f;
+    slope[t] = BIAS ? a.slopes[h] * LOG2E : 0.f;
     const float* qr = (const float*)a.q + (long)(doc.q0 + qi) * a.q_row + h * a.q_head + 4 * kq;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[t][s] = s < KS - 1 || dlast ? *(const f32x4*)(qr + 16 * s) : zero;
@@ -116,8 +117,8 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = kv0 + 16 * c + 4 * kq + e;
-          float z = s[t][c][e] * a.scale;
-          if (CAP) z = a.cap * tanhf(z / a.cap);
+          // the exponent in the exp2 domain
+          float z = CAP ? a.cap * LOG2E * tanhf(s[t][c][e] * (a.scale / a.cap)) : s[t][c][e] * (a.scale * LOG2E);
           if (BIAS) z -= slope[t] * fabsf((float)(here[t] - key));
           s[t][c][e] = masked && key >= lim[t] ? -INFINITY : z;
           mt = fmaxf(mt, s[t][c][e]);
@@ -125,9 +126,9 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
       mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
       mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
       const float m_new = fmaxf(m_run[t], mt);
-      // nothing visible so far: exp(-inf - 0) instead of -inf - (-inf)
+      // nothing visible so far: 2^(-inf - 0) instead of -inf - (-inf)
       const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = expf(m_run[t] - m_ref);
+      const float alpha = __builtin_amdgcn_exp2f(m_run[t] - m_ref);
       m_run[t] = m_new;
       l_run[t] *= alpha;
 #pragma unroll
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[t][c][e] = expf(s[t][c][e] - m_ref);
+          s[t][c][e] = __builtin_amdgcn_exp2f(s[t][c][e] - m_ref);
           l_run[t] += s[t][c][e];
         }
     }
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
                                                            o[t][v], 0, 0, 0);
   }
 
-  // Merge of the four waves: with m = max_w m_w and f_w = exp(m_w - m),
+  // Merge of the four waves: with m = max_w m_w and f_w = 2^(m_w - m),
   // O = sum_w f_w O_w, l = sum_w f_w l_w (a wave without keys has m = -inf
   // and zeros).
 #pragma unroll
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
     f32x4 num = zero;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = expf(ml[w][0][qr] - mr);
+      const float f = __builtin_amdgcn_exp2f(ml[w][0][qr] - mr);
       den += f * ml[w][1][qr];
       num += f * *(const f32x4*)&os[w][qr][d];
     }
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(256) void doc_attn_f32_kernel(DocAttnArgs a) {
     if (a.split > 1) {
       float* pr = a.part + ((long)part * a.q_rows * a.H + (long)(doc.q0 + qi) * a.H + h) * (DH + 4);
       *(f32x4*)(pr + d) = num;
-      if (d == 0) *(f32x2*)(pr + DH) = f32x2{m * LOG2E, den};  // the merge pass works in the exp2 domain
+      if (d == 0) *(f32x2*)(pr + DH) = f32x2{m, den};
     } else {
       *(f32x4*)((float*)a.o + (long)(doc.q0 + qi) * a.o_row + h * a.o_head + d) = num * (den == 0.f ? 0.f : 1.0f / den);
     }

@@ -11,24 +11,20 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct Doc {
   int q0, nq, k0, nk, prefix;
 };
+// The arrays' entries are requested at once (an absent array's from q, and not
+// used): one after the other they would cost a memory round trip each.
 __device__ __forceinline__ Doc load_doc(const DocAttnArgs& a, int d) {
+  const int32_t* none = (const int32_t*)a.q;
+  const int32_t *qs = a.q_start ? a.q_start + d : none, *ks = a.k_start ? a.k_start + d : none;
+  const int32_t *kl = a.k_len ? a.k_len + d : none, *px = a.prefix ? a.prefix + d : none;
+  const int q_lo = qs[0], q_hi = qs[1], k_lo = ks[0], k_hi = ks[1], len = kl[0], pre = px[0];
   Doc o;
-  if (a.q_start) {
-    o.q0 = min(max(a.q_start[d], 0), a.q_rows);
-    o.nq = min(max(min(a.q_start[d + 1], a.q_rows) - o.q0, 0), a.max_q);
-  } else {
-    o.q0 = (int)min((long)d * a.room_q, (long)a.q_rows);
-    o.nq = min(a.max_q, a.q_rows - o.q0);
-  }
-  if (a.k_start) {
-    o.k0 = min(max(a.k_start[d], 0), a.k_rows);
-    o.nk = min(max(min(a.k_start[d + 1], a.k_rows) - o.k0, 0), a.max_k);
-  } else {
-    o.k0 = (int)min((long)d * a.room_k, (long)a.k_rows);
-    o.nk = min(a.max_k, a.k_rows - o.k0);
-  }
-  if (a.k_len) o.nk = min(o.nk, max(a.k_len[d], 0));
-  o.prefix = a.prefix ? min(max(a.prefix[d], 0), o.nk) : 0;
+  o.q0 = a.q_start ? min(max(q_lo, 0), a.q_rows) : (int)min((long)d * a.room_q, (long)a.q_rows);
+  o.nq = min(a.q_start ? max(min(q_hi, a.q_rows) - o.q0, 0) : a.q_rows - o.q0, a.max_q);
+  o.k0 = a.k_start ? min(max(k_lo, 0), a.k_rows) : (int)min((long)d * a.room_k, (long)a.k_rows);
+  o.nk = min(a.k_start ? max(min(k_hi, a.k_rows) - o.k0, 0) : a.k_rows - o.k0, a.max_k);
+  if (a.k_len) o.nk = min(o.nk, max(len, 0));
+  o.prefix = a.prefix ? min(max(pre, 0), o.nk) : 0;
   return o;
 }
 // Keys visible to query i: j < row_limit.  It never falls as i grows.

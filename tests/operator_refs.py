@@ -25,31 +25,32 @@ def attention(q, k, v, scale, mask="full", prefix=0, cap=0.0, slopes=None, dtype
     o, tol = np.zeros(q.shape), np.zeros(q.shape)
     lim = row_limits(nq, nk, mask, prefix)
     u = U[dtype]
+    seen = np.arange(nk)[None, :] < lim[:, None]
+    some = lim > 0
+    if not some.any():
+        return o, tol
     for h in range(H):
         kh, vh = k[:, h * Hk // H], v[:, h * Hk // H]
-        for i in range(nq):
-            n = int(lim[i])
-            if n == 0:
-                continue
-            s = kh[:n] @ q[i, h] * scale
-            mag = np.abs(kh[:n]) @ np.abs(q[i, h]) * scale
-            # fp32 products and sums of a score, the tanh, the bias, the exp
-            eps = mag * (dh + 16) * 2.0 ** -24 + np.abs(s) * 2.0 ** -22
-            if cap > 0:
-                s = cap * np.tanh(s / cap)
-                eps = eps + cap * 2.0 ** -20
-            if slopes is not None:
-                b = slopes[h] * np.abs(i + nk - nq - np.arange(n))
-                s = s - b
-                eps = eps + b * 2.0 ** -22
-            top = s.max()
-            p = np.exp(s - top)
-            # a probability's relative error: its score's, that of the running maximum, its rounding
-            # (to bf16 for the product with v) and the fp32 sums' over n terms
-            rel = np.expm1(eps + eps[s.argmax()]) + 2.0 ** -21 + (u if dtype == "bf16" else 0) + n * 2.0 ** -24
-            w = p / p.sum()
-            o[i, h] = w @ vh[:n]
-            tol[i, h] = 2 * (w * rel) @ np.abs(vh[:n]) + (w @ rel) * np.abs(o[i, h]) + u * np.abs(o[i, h]) + 1e-30
+        s = q[:, h] @ kh.T * scale
+        # fp32 products and sums of a score, the tanh, the bias, the exp
+        eps = (np.abs(q[:, h]) @ np.abs(kh).T * scale) * (dh + 16) * 2.0 ** -24 + np.abs(s) * 2.0 ** -22
+        if cap > 0:
+            s = cap * np.tanh(s / cap)
+            eps += cap * 2.0 ** -20
+        if slopes is not None:
+            b = slopes[h] * np.abs(np.arange(nq)[:, None] + nk - nq - np.arange(nk))
+            s = s - b
+            eps += b * 2.0 ** -22
+        s = np.where(seen, s, -np.inf)[some]
+        at = s.argmax(1)[:, None]
+        p = np.exp(s - np.take_along_axis(s, at, 1))
+        # a probability's relative error: its score's, that of the running maximum, its rounding
+        # (to bf16 for the product with v) and the fp32 sums' over the visible terms
+        rel = np.expm1(eps[some] + np.take_along_axis(eps[some], at, 1)) + 2.0 ** -21 + (u if dtype == "bf16" else 0) \
+            + lim[some, None] * 2.0 ** -24
+        w = p / p.sum(1, keepdims=True)
+        o[some, h] = w @ vh
+        tol[some, h] = 2 * (w * rel) @ np.abs(vh) + ((w * rel).sum(1)[:, None] + u) * np.abs(o[some, h]) + 1e-30
     return o, tol
 
 

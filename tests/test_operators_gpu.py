@@ -120,6 +120,50 @@ def test_attention_long_rows(dtype, dh):
     a.check()
 
 
+# Grids that the kernel of few rows does not take: 256-row workgroups, several key tiles seen whole by all of their
+# rows (one to five: the ring's slots in every turn), tiles on the diagonal and past the end.
+WIDE = [
+    dict(ql=[300, 1, 513, 64, 130, 0, 70], kl=[300, 1, 513, 64, 130, 0, 70]),
+    dict(ql=[300, 1, 513, 64, 130], kl=[300, 1, 513, 64, 130], mask="causal"),
+    dict(ql=[320, 257, 448], kl=[320, 257, 448], mask="prefix", prefix=[64, 257, 200]),
+    dict(ql=[400, 400, 400], kl=[65, 128, 390], room=400, cap=5.0),
+    dict(ql=[700, 380], kl=[700, 380], mask="causal", cap=30.0, bias=True, std=2.0),
+    dict(ql=[1100], kl=[1100], bias=True),
+    dict(ql=[900, 200], kl=[900, 200], mask="causal", std=4.0),
+]
+
+
+@pytest.mark.parametrize("heads", [(24, 24), (24, 8)], ids=lambda h: f"h{h[0]}k{h[1]}")
+@pytest.mark.parametrize("dh", [64, 72, 128])
+@pytest.mark.parametrize("case", range(len(WIDE)))
+def test_attention_many_rows(case, dh, heads):
+    a = Attn("bf16", heads[0], heads[1], dh, **WIDE[case], seed=7 * case + dh)
+    a.run()
+    a.check()
+
+
+@pytest.mark.parametrize("dh", [64, 72, 128])
+def test_attention_many_rows_what_is_not_visible_does_not_count(dh):
+    """As test_attention_what_is_not_visible_does_not_count, for the kernel of many rows: a document's padding, the
+    next document's keys and the keys above the diagonal."""
+    a = Attn("bf16", 24, 24, dh, [600, 333], [590, 333], room=600, mask="causal", seed=3, fused=False)
+    b = Attn("bf16", 24, 24, dh, [600, 333], [590, 333], room=600, mask="causal", seed=3, fused=False)
+    for t in (a.k, a.v):
+        for lo, hi in ((590, 600), (933, 1200)):
+            t[lo:hi:3], t[lo + 1:hi:3], t[lo + 2:hi:3] = float("nan"), float("inf"), float("-inf")
+    a.run()
+    b.run()
+    assert torch.equal(a.o, b.o)
+    a.check()
+    # a visible NaN value and infinity: exactly the rows that see their key, in their column
+    a.v[700, 5, 9], a.v[801, 6, 10] = float("nan"), float("inf")
+    a.run()
+    got, want = a.o[600:933].clone(), b.o[600:933]
+    assert got[100:, 5, 9].isnan().all() and (got[201:, 6, 10] == float("inf")).all()
+    got[100:, 5, 9], got[201:, 6, 10] = want[100:, 5, 9], want[201:, 6, 10]
+    assert torch.equal(got, want) and torch.equal(a.o[:600], b.o[:600])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_uniform_rooms_need_no_starts(dtype):
     a = Attn(dtype, 4, 2, 64, [50, 50, 50], [33, 50, 0], room=50, mask="full")
@@ -290,9 +334,13 @@ LINEAR = [(1, 16, 1), (1, 1152, 6912), (3, 144, 40), (8, 1152, 136), (16, 4608, 
           (130, 1152, 384), (257, 272, 1000), (300, 64, 520), (128, 128, 128), (640, 1536, 768)]
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32", "e4m3"])
-@pytest.mark.parametrize("act", ["none", "gelu"])
-@pytest.mark.parametrize("M,K,N", LINEAR)
+# ... and what the large tiles take: whole, and with the last round's tiles divided over k; a last block of 16
+LARGE = [(1900, 272, 4400, "gelu", "e4m3"), (1900, 272, 4400, "none", "bf16"), (1901, 128, 4501, "gelu", "bf16"),
+         (4500, 1040, 4400, "none", "e4m3"), (4500, 1040, 4400, "gelu", "bf16"), (1900, 272, 4400, "none", "f32"),
+         (1030, 4608, 1160, "gelu", "f32"), (1030, 4608, 1160, "gelu", "e4m3")]
+
+
+@pytest.mark.parametrize("M,K,N,act,dtype", [(*s, a, d) for s in LINEAR for a in ("none", "gelu") for d in ("bf16", "f32", "e4m3")] + LARGE)
 def test_linear(M, K, N, act, dtype):
     if dtype == "e4m3" and N % 8:
         N = -(-N // 8) * 8
