@@ -460,10 +460,13 @@ __global__ __launch_bounds__(256) void linear_f8_finish_kernel(LinF8Args a) {
 // tiles of 256 x 256 (one workgroup per CU; not for fp32 outputs, whose widened
 // operands need the registers) or 128 x 128 (two per CU), the last round's tiles
 // divided over k into up to eight ranges, by the least estimate of
-//   4 us a round + (blocks of k) x 1.82 us for a round of 256 large tiles, 1.4 us
-//   of up to 512 small ones, 0.8 us of up to 256; 6 us for adding ranges up
-// (measured at 1024 .. 17550 rows; ranges of two blocks did not pay: 1024 x 1152
-// x 1152 23 us in four ranges, 10.6 us whole; 1024 x 4608 x 1152 25 against 32).
+//   11 us a round + 1.85 us a block of k for 256 large tiles,
+//   4 us a round + 1.3 us a block for up to 512 small ones (0.7 us for up to 256),
+//   6 us (small tiles) or 10 us for adding ranges up
+// (measured at 1024 .. 17550 rows: 8192 x 1152 x 4608 73 us in small tiles, 83 in
+// large ones; 16384 x 8192 x 4096 645 and 515.  Ranges of two blocks did not pay:
+// 1024 x 1152 x 1152 23 us in four ranges, 10.1 us whole; 1024 x 4608 x 1152 25
+// against 32).
 LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
   LinF8Plan p{};
   p.split = 1;
@@ -477,8 +480,9 @@ LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
     const long t = (long)((M + tile - 1) / tile) * ((N + tile - 1) / tile), slots = tile == 256 ? 256 : 512;
     const long full = t / slots, rem = t % slots;
     for (int s = 1; s <= 8 && (s == 1 || (KB >= 4 * s && rem * s <= slots && rem > 0)); ++s) {
-      const double block = tile == 256 ? 1.82 : 1.4, part = tile == 128 && rem * s <= 256 ? 0.8 : block;
-      const double us = full * (4 + KB * block) + (rem ? 4 + KB * part / s + (s > 1 ? 6 : 0) : 0);
+      const double round = tile == 256 ? 11 : 4, block = tile == 256 ? 1.85 : 1.3;
+      const double part = tile == 128 && rem * s <= 256 ? 0.7 : block;
+      const double us = full * (round + KB * block) + (rem ? round + KB * part / s + (s == 1 ? 0 : tile == 256 ? 10 : 6) : 0);
       if (p.tile != 0 && us >= best) continue;
       best = us;
       p.tile = tile;
@@ -522,7 +526,7 @@ static void launch_out(const LinF8Args& a, int tile, hipStream_t st) {
   if constexpr (OUT != 0) {
     if (tile == 256) return launch_tile<256, 256, 4, 2, OUT>(a, st);
   }
-  launch_tile<128, 128, 2, 2, OUT>(a, st);
+  launch_tile<128, 128, 4, 2, OUT>(a, st);
 }
 
 hipError_t launch_linear_fp8(const LinF8Args& a, int tile, hipStream_t st) {
