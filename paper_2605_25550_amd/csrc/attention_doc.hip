@@ -34,34 +34,42 @@ template <int DH>
 struct DocCfg {
   static constexpr int DHP = (DH + 15) / 16 * 16;
   static constexpr int BKV = 64;
-  static constexpr int ROW = DHP * 2;            // bytes per K or V row in LDS
-  static constexpr int CPR = ROW / 16;           // 16-byte chunks per row ...
-  static constexpr int RC = DH / 8;              // ... of which hold data
-  static constexpr int TILE = BKV * ROW;         // bytes of a K or V tile
+  static constexpr int ROW = DHP * 2;            // bytes per K row in LDS ...
+  // ... and per V row: a transposed read takes 64 bytes of each of four
+  // consecutive rows, which 192 bytes (unlike 160) send to different banks
+  static constexpr int VROW = DHP == 80 ? 192 : ROW;
+  static constexpr int RC = DH / 8;              // 16-byte chunks of a row that hold data
+  static constexpr int TILE = BKV * ROW, VTILE = BKV * VROW;  // bytes of a K, a V tile
   static constexpr int DT = (DH + 31) / 32;      // 32-row tiles of O^T
   static constexpr int KS = DHP / 16;
-  static constexpr int DMA = TILE / 1024;        // DMA instructions of a K or V tile
+  static constexpr int KDMA = TILE / 1024, VDMA = VTILE / 1024;  // DMA instructions of a K, a V tile
   static constexpr int ST = 4;                   // ring slots: the K tiles of all, then the V tiles
   // head_dim 72: V's pad column 72 holds ones, so that O^T row 72 is the row sum
-  static constexpr bool FOLD = CPR > RC;
+  static constexpr bool FOLD = DHP > DH;
   static constexpr int LT = DH / 32, LG = (DH % 32) % 8 / 4, LE = (DH % 32) / 8 * 4 + DH % 4;
   // stored position of 16-byte chunk c of K row r / V row r
   static __device__ __forceinline__ int pos_k(int r, int c) {
     return c ^ (DHP == 128 ? (r & 15) : (DHP == 64 ? ((r >> 1) & 7) : ((r >> 3) & 1)));
   }
-  // A transposed read takes 64 bytes of each of four consecutive rows: they
-  // go to different quarters of the 64 banks.
+  // (a transposed read's four rows in different quarters of the 64 banks)
   static __device__ __forceinline__ int pos_v(int r, int c) {
     return c ^ (DHP == 128 ? (r & 3) << 2 : (DHP == 64 ? ((r >> 1) & 1) << 2 : 0));
   }
-  static_assert(TILE % 1024 == 0 && ST * TILE <= 65536, "whole DMA blocks; slot offsets fit the LDS immediate");
+  static_assert(TILE % 1024 == 0 && VTILE % 1024 == 0 && ST * VTILE <= 65536, "whole DMA blocks; slot offsets fit the LDS immediate");
 };
+
+// Holds a value's computation where it is written: the compiler orders pure
+// arithmetic by its uses, past the scheduling barriers between matrix products.
+__device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
 
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 __device__ __forceinline__ s16x4 read_tr(const lds_byte* p) {
   typedef __attribute__((address_space(3))) s16x4* lds_p;
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p);
 }
+
+// The pad chunk (columns 72 .. 79) of head_dim 72's K rows, and of its V rows.
+__device__ const uint32_t doc_pads[8] = {0u, 0u, 0u, 0u, 0x3F80u, 0u, 0u, 0u};
 
 // A row's scores, raw -> z (the exponent in the exp2 domain) -> probability.  The
 // scale and the cap keep the order of scores, so that they can wait for the
@@ -99,7 +107,7 @@ __device__ __forceinline__ void clean_v(int (&bad)[3][DH], unsigned char* vt, in
   constexpr int N = C::BKV * C::RC, PER = (N + NT - 1) / NT;
   auto at = [&](int i) {
     const int e = min(t + i * NT, N - 1), R = e / C::RC, c = e - R * C::RC;
-    return (bf16_t*)(vt + R * C::ROW + C::pos_v(R, c) * 16);
+    return (bf16_t*)(vt + R * C::VROW + C::pos_v(R, c) * 16);
   };
   uint32_t odd = 0;
 #pragma unroll
@@ -120,11 +128,12 @@ template <int DH, int NW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a) {
   using C = DocCfg<DH>;
   constexpr int ST = C::ST, BM = NW * 32;
-  constexpr int IPW = (2 * C::DMA + NW - 1) / NW;  // DMA instructions per wave and tile (uniform)
-  constexpr bool SPARE = IPW * NW > 2 * C::DMA;
+  constexpr int NDMA = C::KDMA + C::VDMA, IPW = (NDMA + NW - 1) / NW;  // DMA instructions per wave and tile (uniform)
+  constexpr bool SPARE = IPW * NW > NDMA;
+  constexpr int VBASE = ST * C::TILE, SPARE_AT = VBASE + ST * C::VTILE;
   // the ring, then a line that absorbs spare DMAs (and what transposed reads of
   // head_dim 72 touch past the last V row)
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * ST * C::TILE + 1024];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[ST * (C::TILE + C::VTILE) + 1024];
   __shared__ int bad[3][DH];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -162,11 +171,13 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
   for (int s = 0; s < C::KS; ++s)
     qf[s] = s * 16 + g * 8 < DH ? *(const bf16x8*)(qp + s * 16 + g * 8) : bf16x8{};
 
-  // DMA of one tile into its slot: instruction i < DMA covers K bytes
-  // [1024 i, +1024), the next DMA the V bytes; wave w issues i = w + NW t.  The
+  // DMA of one tile into its slot: instruction i < KDMA covers K bytes
+  // [1024 i, +1024), the next VDMA the V bytes; wave w issues i = w + NW t.  The
   // source is a scalar base (the tile's first row) plus a 32-bit lane offset;
-  // the last tile's rows past the document's end repeat its last row.  The pad
-  // chunk of head_dim 72's rows is no lane's: it keeps what is written below.
+  // the last tile's rows past the document's end repeat its last row.  Head_dim
+  // 72's pad chunks come from doc_pads: a select, because a branch around the copy
+  // (lanes switched off) would end the basic block, and the compiler would sink
+  // the exponentials out of the products they are meant to run beside.
   // Past the last tile, and for spare instructions, the copy goes to the spare
   // line, so that every wave counts the same.
   const int kv_last = (t1 - 1) * C::BKV;  // (some of its rows may lie past the end)
@@ -175,32 +186,30 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
 #pragma unroll
   for (int t = 0; t < IPW; ++t) {
     const int i = wave + NW * t;  // wave-uniform
-    const bool real = !SPARE || i < 2 * C::DMA, isv = real && i >= C::DMA;
-    const int byte = (isv ? i - C::DMA : real ? i : 0) * 1024 + lane * 16;
-    const int R = byte / C::ROW, pos = (byte % C::ROW) >> 4, c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
+    const bool real = !SPARE || i < NDMA, isv = real && i >= C::KDMA;
+    const int byte = (isv ? i - C::KDMA : real ? i : 0) * 1024 + lane * 16, pitch = isv ? C::VROW : C::ROW;
+    const int R = byte / pitch, pos = (byte - R * pitch) >> 4, c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
     const unsigned rs = (unsigned)(isv ? a.v_row : a.k_row) * 2;
     off[t] = R * rs + c * 16;
     off_last[t] = min(R, doc.nk - 1 - kv_last) * rs + c * 16;
-    copies[t] = C::CPR == C::RC || c < C::RC;
+    copies[t] = !C::FOLD || c < C::RC;
   }
   auto issue_one = [&](int tile, int slot, int t) {
     const int i = wave + NW * t;
-    const bool real = !SPARE || i < 2 * C::DMA, isv = real && i >= C::DMA;
+    const bool real = !SPARE || i < NDMA, isv = real && i >= C::KDMA;
     const int tl = min(tile, t1 - 1);
     const bf16_t* base = isv ? vp + (long)(tl * C::BKV) * a.v_row : kp + (long)(tl * C::BKV) * a.k_row;
-    const unsigned dst = real && tile < t1 ? lds0 + (isv ? (ST + slot) * C::TILE + (i - C::DMA) * 1024 : slot * C::TILE + i * 1024)
-                                           : lds0 + 2 * ST * C::TILE;
-    if (copies[t]) dma_16s(base, tl == t1 - 1 ? off_last[t] : off[t], dst);
+    const unsigned dst = real && tile < t1 ? lds0 + (isv ? VBASE + slot * C::VTILE + (i - C::KDMA) * 1024 : slot * C::TILE + i * 1024)
+                                           : lds0 + SPARE_AT;
+    const unsigned o = tl == t1 - 1 ? off_last[t] : off[t];
+    if (C::FOLD)
+      dma_16(copies[t] ? (const void*)((const char*)base + o) : (const void*)(doc_pads + (isv ? 4 : 0)), dst);
+    else
+      dma_16s(base, o, dst);
   };
   for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
-  if (C::FOLD) {
-    for (int e = tid; e < 256; e += NW * 64) ((uint32_t*)(smem + 2 * ST * C::TILE))[e] = 0;
-    for (int e = tid; e < 2 * ST * C::BKV * 4; e += NW * 64) {
-      const int R = (e >> 2) & (C::BKV - 1), tile = e >> 8;  // K tiles, then V tiles
-      const int pos = tile >= ST ? C::pos_v(R, C::RC) : C::pos_k(R, C::RC);
-      ((uint32_t*)(smem + tile * C::TILE + R * C::ROW + pos * 16))[e & 3] = tile >= ST && (e & 3) == 0 ? 0x3F80u : 0u;
-    }
-  }
+  if (C::FOLD)
+    for (int e = tid; e < 256; e += NW * 64) ((uint32_t*)(smem + SPARE_AT))[e] = 0;
 
   const lds_byte* k_at[C::KS];
 #pragma unroll
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     const int R = 4 * g + ((lane & 15) >> 2), half = (lane >> 4) & 1;
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
-      v_at[t] = (const lds_byte*)smem + ST * C::TILE + R * C::ROW +
+      v_at[t] = (const lds_byte*)smem + VBASE + R * C::VROW +
                 (C::pos_v(R, t * 4 + half * 2 + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
   }
   auto kread = [&](int slot, int kt, int s) {
@@ -219,8 +228,8 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
   // keys 16 c + 4 g + 0..3 and 16 c + 8 + 4 g + 0..3 of column 32 t + r32: the
   // keys of the lane's probabilities
   auto vread = [&](int slot, int c, int t) {
-    const lds_byte* p = v_at[t] + slot * C::TILE + c * 16 * C::ROW;
-    const u32x2 lo = __builtin_bit_cast(u32x2, read_tr(p)), hi = __builtin_bit_cast(u32x2, read_tr(p + 8 * C::ROW));
+    const lds_byte* p = v_at[t] + slot * C::VTILE + c * 16 * C::VROW;
+    const u32x2 lo = __builtin_bit_cast(u32x2, read_tr(p)), hi = __builtin_bit_cast(u32x2, read_tr(p + 8 * C::VROW));
     return u32x4{lo[0], lo[1], hi[0], hi[1]};
   };
 
@@ -290,7 +299,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     // the slot behind it: computed, and not used.)
     auto tile_step = [&](const int j, const int sj, f32x16 (&scur)[2], f32x16 (&snext)[2]) __attribute__((always_inline)) {
       lead(score.z_of_max(mcur));
-      constexpr int EX = C::FOLD ? 16 : 24;  // exponentials beside QK^T; the rest beside the first PV MFMAs
+      constexpr int EX = C::FOLD || CAP ? 16 : 24;  // exponentials beside QK^T; the rest beside the first PV MFMAs
       constexpr int NP = 4 * C::DT, NPRE = EX / 8 * C::DT, ND = 3, NQ = 2 * C::KS;
       u32x4 pw[4], vf[3];
       auto pack = [&](int p) { pw[p >> 2][p & 3] = pack_bf16x2(scur[p >> 3][(2 * p) & 15], scur[p >> 3][(2 * p + 1) & 15]); };
@@ -306,7 +315,11 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
           if (i == NQ - 2) vf[0] = vread(sj, 0, 0);
           if (i == NQ - 1) vf[1] = vread(sj, 1 / C::DT, 1 % C::DT);
 #pragma unroll
-          for (int e = i * EX / NQ; e < (i + 1) * EX / NQ; ++e) scur[e >> 4][e & 15] = prob(scur[e >> 4][e & 15]);
+          for (int e = i * EX / NQ; e < (i + 1) * EX / NQ; ++e) {
+            float x = prob(scur[e >> 4][e & 15]);
+            pin(x);
+            scur[e >> 4][e & 15] = x;
+          }
 #pragma unroll
           for (int p = 0; p < EX / 2; ++p)
             if (2 * p + 1 >= i * EX / NQ && 2 * p + 1 < (i + 1) * EX / NQ) pack(p);
@@ -328,10 +341,15 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
             snext[e >> 4][e & 15] = pre(snext[e >> 4][e & 15], first, e >> 4, e & 15);
             m = fmaxf(m, snext[e >> 4][e & 15]);
           }
+          if (i % 4 == 3) pin(m);
           if (i < NPRE) {
 #pragma unroll
             for (int e = EX + i * (32 - EX) / NPRE; e < EX + (i + 1) * (32 - EX) / NPRE; ++e)
-              scur[e >> 4][e & 15] = prob(scur[e >> 4][e & 15]);
+            {
+              float x = prob(scur[e >> 4][e & 15]);
+              pin(x);
+              scur[e >> 4][e & 15] = x;
+            }
 #pragma unroll
             for (int p = EX / 2; p < 16; ++p)
               if (2 * p + 1 >= EX + i * (32 - EX) / NPRE && 2 * p + 1 < EX + (i + 1) * (32 - EX) / NPRE) pack(p);
@@ -372,7 +390,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     wait_vmcnt<0>();
     __syncthreads();
     for (int t = 0; t < IPW; ++t) issue_one(it + ST - 1, (slot + ST - 1) % ST, t);
-    clean_v<DH, NW * 64>(bad, smem + (ST + slot) * C::TILE, kv0, tid);
+    clean_v<DH, NW * 64>(bad, smem + VBASE + slot * C::VTILE, kv0, tid);
     f32x16 s[2];
     float m = -INFINITY;
     const float first = score.here - (float)(kv0 + 4 * g);
@@ -465,7 +483,7 @@ template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   using C = DocCfg<DH>;
   constexpr int NW = 4, OS = DH + 4;
-  constexpr int RING = 2 * C::TILE + 256;  // of one wave (+ what transposed reads of head_dim 72 touch past V)
+  constexpr int RING = C::TILE + C::VTILE + 256;  // of one wave (+ what transposed reads of head_dim 72 touch past V)
   static_assert(NW * RING >= NW * 32 * OS * 4, "the states are merged where the rings were");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * RING];
   __shared__ float ml[NW][2][32];
@@ -496,11 +514,12 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     const long rs = isv ? a.v_row : a.k_row;
     const bf16_t* base = (isv ? vp : kp) + (long)kv0 * rs;
 #pragma unroll
-    for (int i = 0; i < C::DMA; ++i) {
-      const int byte = i * 1024 + lane * 16, R = byte / C::ROW, pos = (byte % C::ROW) >> 4;
+    for (int i = 0; i < (C::VDMA > C::KDMA ? C::VDMA : C::KDMA); ++i) {
+      if (i >= (isv ? C::VDMA : C::KDMA)) break;
+      const int byte = i * 1024 + lane * 16, pitch = isv ? C::VROW : C::ROW, R = byte / pitch, pos = (byte - R * pitch) >> 4;
       const int c = isv ? C::pos_v(R, pos) : C::pos_k(R, pos);
       const unsigned off = (unsigned)min(R, doc.nk - 1 - kv0) * (unsigned)(rs * 2) + c * 16;
-      if (C::CPR == C::RC || c < C::RC) dma_16s(base, off, lds0 + (isv ? C::TILE : 0) + i * 1024);
+      if (!C::FOLD || c < C::RC) dma_16s(base, off, lds0 + (isv ? C::TILE : 0) + i * 1024);
     }
   };
   if (t0 + wave < t1) {
@@ -512,12 +531,12 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   for (int s = 0; s < C::KS; ++s)
     qf[s] = s * 16 + g * 8 < DH ? *(const bf16x8*)(qp + s * 16 + g * 8) : bf16x8{};
   for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
-  if (C::CPR > C::RC) {
-    ((uint32_t*)(ring + 2 * C::TILE))[lane] = 0;
-    for (int e = lane; e < 2 * C::BKV * 4; e += 64) {
-      const int R = (e >> 2) & (C::BKV - 1), isv = e >> 8;
-      ((uint32_t*)(ring + isv * C::TILE + R * C::ROW + (isv ? C::pos_v(R, C::RC) : C::pos_k(R, C::RC)) * 16))[e & 3] = 0;
-    }
+  if (C::FOLD) {  // the pad chunks are no lane's: K's must be zero, V's (discarded columns) are
+    ((uint32_t*)(ring + C::TILE + C::VTILE))[lane] = 0;
+    for (int e = lane; e < C::BKV * 4; e += 64)
+      ((uint32_t*)(ring + (e >> 2) * C::ROW + C::pos_k(e >> 2, C::RC) * 16))[e & 3] = 0;
+    for (int e = lane; e < C::BKV * 12; e += 64)
+      ((uint32_t*)(ring + C::TILE + e / 12 * C::VROW + C::RC * 16))[e % 12] = 0;
   }
   __syncthreads();
 
@@ -529,7 +548,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     const int R = 4 * g + ((lane & 15) >> 2), half = (lane >> 4) & 1;
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
-      v_at[t] = (const lds_byte*)ring + C::TILE + R * C::ROW +
+      v_at[t] = (const lds_byte*)ring + C::TILE + R * C::VROW +
                 (C::pos_v(R, t * 4 + half * 2 + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
   }
   const DocScore<CAP, BIAS> score(a, h, qi + doc.nk - doc.nq);
@@ -546,7 +565,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   for (int it = t0 + wave; it < t1; it += NW) {
     const int kv0 = it * C::BKV;
     const bool more = it + NW < t1, masked = kv0 + C::BKV > lim_lo;
-    if (it > t0 + wave) wait_vmcnt<C::DMA>();  // this tile's K (its V, issued behind it, may still be under way)
+    if (it > t0 + wave) wait_vmcnt<C::VDMA>();  // this tile's K (its V, issued behind it, may still be under way)
     f32x16 s[2];
     float m = -INFINITY;
     const float first = score.here - (float)(kv0 + 4 * g);
@@ -588,7 +607,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
         pw[c][w] = pack_bf16x2(x == -INFINITY ? 0.f : score.prob(x, mneg), y == -INFINITY ? 0.f : score.prob(y, mneg));
         l_run += __uint_as_float(pw[c][w] << 16) + __uint_as_float(pw[c][w] & 0xFFFF0000u);
       }
-    if (more) wait_vmcnt<C::DMA>();  // this tile's V (the next K may be under way)
+    if (more) wait_vmcnt<C::KDMA>();  // this tile's V (the next K may be under way)
     else wait_vmcnt<0>();
     if (masked) {
       clean_v<DH, 64>(bad, ring + C::TILE, kv0, lane);
@@ -598,8 +617,8 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int t = 0; t < C::DT; ++t) {
-        const lds_byte* p = v_at[t] + c * 16 * C::ROW;
-        const u32x2 lo = __builtin_bit_cast(u32x2, read_tr(p)), hi = __builtin_bit_cast(u32x2, read_tr(p + 8 * C::ROW));
+        const lds_byte* p = v_at[t] + c * 16 * C::VROW;
+        const u32x2 lo = __builtin_bit_cast(u32x2, read_tr(p)), hi = __builtin_bit_cast(u32x2, read_tr(p + 8 * C::VROW));
         oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]}),
                                                           __builtin_bit_cast(bf16x8, pw[c]), oacc[t], 0, 0, 0);
       }
@@ -749,7 +768,7 @@ hipError_t launch_doc_attn_merge(const DocAttnArgs& a, int head_dim, int dtype, 
 
 // bf16: up to 32 rows of a document and key head, and grids that its 32-row
 // workgroups do not fill (one for each CU; two of head_dim 64), go to the kernel
-// of few rows (one document of 256 tokens, 16 heads of 72: ROWFEW us against 10.6).
+// of few rows (one document of 256 tokens, 16 heads of 72: 8.5 us against 10.6).
 // A grid that leaves compute units idle divides the keys of its items into
 // ranges, of four tiles (256 keys; fp32: 128) at least, until there is a
 // workgroup for each unit (fp32, and few rows of 64: two).  More ranges cost more
