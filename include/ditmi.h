@@ -293,7 +293,7 @@ dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, floa
  *   max_q, max_k     no document has more query rows, or keys (longer ones
  *                    are cut to them)
  *   dtype            of q, k, v and o
- *   scale > 0;  cap >= 0 (0: none)
+ *   scale > 0 (at most 2^100);  cap 0 (none) or in 2^-20 .. 2^12
  *   *_row, *_head    strides in elements between rows and between heads of
  *                    each tensor, multiples of 8 (bf16) or 4 (fp32); the
  *                    head_dim elements of a head are contiguous.  Rows at
@@ -372,7 +372,7 @@ dit_status dit_linear_fp8(const dit_linear_shape *s, const void *a, const float 
  * DIT_NORM_LAYER subtracts the mean and divides by the standard deviation
  * (biased variance), DIT_NORM_RMS divides by the root mean square, both with
  * eps; DIT_NORM_NONE (post only) leaves y as it is.  b = row_batch[row].
- *   rows >= 0, hidden a multiple of 8 in 8 .. 8192
+ *   rows >= 0 (at most 2^25), hidden a multiple of 8 in 8 .. 8192
  *   batch      rows of gate, shift and scale, mod_stride elements apart (a
  *              multiple of 4): slices of one modulation matrix
  *   y_dtype    of y: DIT_F32 or DIT_BF16

@@ -76,13 +76,14 @@ __device__ const uint32_t doc_pads[8] = {0u, 0u, 0u, 0u, 0x3F80u, 0u, 0u, 0u};
 // exponential, after the row max; the bias cannot.
 template <bool CAP, bool BIAS>
 struct DocScore {
-  float sc, cap_in, cap_out, slope, here;
+  float sc, cap_in, cap_out, slope;
+  int here;
   __device__ __forceinline__ DocScore(const DocAttnArgs& a, int h, int place) {
     sc = a.scale * LOG2E;
     cap_in = CAP ? 2.0f * sc / a.cap : 0.f;
     cap_out = CAP ? a.cap * LOG2E : 0.f;
     slope = BIAS ? a.slopes[h] * LOG2E : 0.f;
-    here = (float)place;  // the key at the row's own place
+    here = place;  // the key at the row's own place: distances to it are taken as integers
   }
   // cap tanh(s scale / cap) = cap - 2 cap / (exp(2 s scale / cap) + 1), plus `more`, in the exp2 domain
   __device__ __forceinline__ float capped(float s, float more) const {
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     }
     float mcur = -INFINITY;  // row max of the current tile (what pre() gives), both halves
     {
-      const float first = score.here - (float)(t0 * C::BKV + 4 * g);
+      const float first = (float)(score.here - (t0 * C::BKV + 4 * g));
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
         }
       }
       {
-        const float first = score.here - (float)((j + 1) * C::BKV + 4 * g);
+        const float first = (float)(score.here - ((j + 1) * C::BKV + 4 * g));
         float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -393,7 +394,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     clean_v<DH, NW * 64>(bad, smem + VBASE + slot * C::VTILE, kv0, tid);
     f32x16 s[2];
     float m = -INFINITY;
-    const float first = score.here - (float)(kv0 + 4 * g);
+    const float first = (float)(score.here - (kv0 + 4 * g));
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       s[kt] = f32x16{};
@@ -568,7 +569,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     if (it > t0 + wave) wait_vmcnt<C::VDMA>();  // this tile's K (its V, issued behind it, may still be under way)
     f32x16 s[2];
     float m = -INFINITY;
-    const float first = score.here - (float)(kv0 + 4 * g);
+    const float first = (float)(score.here - (kv0 + 4 * g));
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       s[kt] = f32x16{};

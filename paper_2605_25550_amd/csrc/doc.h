@@ -20,9 +20,9 @@ __device__ __forceinline__ Doc load_doc(const DocAttnArgs& a, int d) {
   const int q_lo = qs[0], q_hi = qs[1], k_lo = ks[0], k_hi = ks[1], len = kl[0], pre = px[0];
   Doc o;
   o.q0 = a.q_start ? min(max(q_lo, 0), a.q_rows) : (int)min((long)d * a.room_q, (long)a.q_rows);
-  o.nq = min(a.q_start ? max(min(q_hi, a.q_rows) - o.q0, 0) : a.q_rows - o.q0, a.max_q);
+  o.nq = min((a.q_start ? min(max(q_hi, o.q0), a.q_rows) : a.q_rows) - o.q0, a.max_q);
   o.k0 = a.k_start ? min(max(k_lo, 0), a.k_rows) : (int)min((long)d * a.room_k, (long)a.k_rows);
-  o.nk = min(a.k_start ? max(min(k_hi, a.k_rows) - o.k0, 0) : a.k_rows - o.k0, a.max_k);
+  o.nk = min((a.k_start ? min(max(k_hi, o.k0), a.k_rows) : a.k_rows) - o.k0, a.max_k);
   if (a.k_len) o.nk = min(o.nk, max(len, 0));
   o.prefix = a.prefix ? min(max(pre, 0), o.nk) : 0;
   return o;

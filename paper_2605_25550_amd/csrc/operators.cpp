@@ -39,12 +39,17 @@ dit_status check_attn(const dit_attn_shape* s) {
   if (s->q_rows < 0 || s->k_rows < 0 || s->max_q < 0 || s->max_k < 0)
     return fail(DIT_ERR_INVALID_ARG, "q_rows (%d), k_rows (%d), max_q (%d), max_k (%d) must be >= 0", s->q_rows,
                 s->k_rows, s->max_q, s->max_k);
-  if ((long)s->max_q * s->heads >= (1L << 30) || (long)s->max_q * s->heads / s->kv_heads >= (1L << 24) ||
+  // (a grid has fewer than 2^32 threads: 16 for each query and head in fp32)
+  if ((long)s->max_q * s->heads >= (s->dtype == DIT_BF16 ? 1L << 30 : 1L << 27) || (long)s->max_q * s->heads / s->kv_heads >= (1L << 24) ||
       s->max_k >= (1 << 30) || s->k_rows >= (1 << 30) || s->q_rows >= (1 << 30))
     return fail(DIT_ERR_UNSUPPORTED, "documents of %d queries and %d keys, or %d / %d rows, are too long", s->max_q,
                 s->max_k, s->q_rows, s->k_rows);
   if (!(s->scale > 0.f) || !isfinite(s->scale) || !(s->cap >= 0.f) || !isfinite(s->cap))
     return fail(DIT_ERR_INVALID_ARG, "scale (%g) must be finite and > 0, cap (%g) finite and >= 0", s->scale, s->cap);
+  // past these the scale times a score of 0 would be inf * 0, and the tanh's fp32
+  // arithmetic (an error of cap * 2^-20 in a score) coarser than the probabilities
+  if (s->scale > 0x1p100f || (s->cap > 0.f && (s->cap < 0x1p-20f || s->cap > 0x1p12f)))
+    return fail(DIT_ERR_UNSUPPORTED, "scale (%g) > 2^100, or cap (%g) not 0 and not in 2^-20 .. 2^12", s->scale, s->cap);
   const int unit = s->dtype == DIT_BF16 ? 8 : 4, dh = s->head_dim;
   dit_status st;
   if ((st = check_strides("q", s->q_row, s->q_head, s->heads, s->q_rows, dh, unit)) != DIT_OK) return st;
@@ -186,7 +191,9 @@ dit_status dit_quantize_fp8(int32_t rows, int32_t cols, int32_t block_rows, int3
                 rows, cols, (long long)x_row);
   if (block_rows != 1 && block_rows != 128) return fail(DIT_ERR_INVALID_ARG, "block_rows (%d) must be 1 or 128", block_rows);
   if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d unknown", dtype);
-  if (x_row > (1L << 40) || (long)rows > 65535L * 128 || ((long)rows * ((cols + 127) / 128) + 15) / 16 >= (1L << 31))
+  // (a grid has fewer than 2^32 threads: 16 for a block of one row, 256 for one of 128 rows)
+  const long blocks = (long)rows * (((long)cols + 127) / 128);
+  if (x_row > (1L << 40) || cols > (1 << 30) || (block_rows == 1 ? blocks >= (1L << 28) - 16 : rows > 65535 * 128))
     return fail(DIT_ERR_UNSUPPORTED, "%d rows of %d columns are too many", rows, cols);
   if (rows == 0) return DIT_OK;
   TRY(check_ptr(x, "x", 16, false));
@@ -250,7 +257,8 @@ dit_status dit_norm_residual(const dit_norm_shape* s, const float* x, float* x_o
   if (s->rows < 0 || s->hidden < 8 || s->hidden % 8 != 0 || s->batch < 1)
     return fail(DIT_ERR_INVALID_ARG, "rows (%d) must be >= 0, hidden (%d) a positive multiple of 8, batch (%d) >= 1",
                 s->rows, s->hidden, s->batch);
-  if (s->hidden > 8192) return fail(DIT_ERR_UNSUPPORTED, "hidden %d > 8192 is not supported", s->hidden);
+  if (s->hidden > 8192 || s->rows > (1 << 25))  // (a grid has fewer than 2^32 threads: 64 for a row)
+    return fail(DIT_ERR_UNSUPPORTED, "%d rows of %d: more than 2^25 rows or 8192 columns are not supported", s->rows, s->hidden);
   if (s->post < DIT_NORM_NONE || s->post > DIT_NORM_RMS || s->pre < DIT_NORM_LAYER || s->pre > DIT_NORM_RMS)
     return fail(DIT_ERR_INVALID_ARG, "norms (post %d, pre %d) unknown", s->post, s->pre);
   if ((s->y_dtype != DIT_F32 && s->y_dtype != DIT_BF16) || s->h_dtype < DIT_F32 || s->h_dtype > DIT_E4M3)

@@ -40,6 +40,8 @@ def call_attn(dm, s, q=P, k=P, v=P, o=P, q_start=P, k_start=P, k_len=None, prefi
     (dict(scale=float("nan")), BAD), (dict(scale=float("inf")), BAD), (dict(cap=-1.0), BAD), (dict(cap=float("nan")), BAD),
     (dict(q_row=516), BAD), (dict(k_head=60), BAD), (dict(v_row=-128), BAD), (dict(o_row=32), BAD), (dict(k_head=56), BAD),
     (dict(k_row=1 << 23), UNSUP), (dict(max_q=1 << 28, q_rows=1 << 29), UNSUP), (dict(k_rows=1 << 30), UNSUP),
+    (dict(scale=2e38), UNSUP), (dict(cap=1e-30), UNSUP), (dict(cap=1e4), UNSUP),
+    (dict(dtype=0, max_q=1 << 24, q_rows=1 << 24), UNSUP),
 ])
 def test_attention_shapes(dm, kw, want):
     s = attn(dm, **kw)
@@ -84,6 +86,8 @@ def test_quantize(dm):
                dict(x=None), dict(x=P + 4), dict(codes=None), dict(codes=P + 1), dict(scale=None), dict(scale=P + 2)):
         assert call(**kw) == BAD, kw
     assert call(rows=70000 * 128, block=128) == UNSUP
+    assert call(rows=1 << 28) == UNSUP and call(rows=1 << 20, cols=1 << 16, row=1 << 16) == UNSUP
+    assert call(rows=1, cols=(1 << 30) + 8, row=1 << 31, block=128) == UNSUP
     assert call(rows=0, x=None, codes=None, scale=None) == 0
 
 
@@ -125,7 +129,7 @@ def test_norm(dm):
                dict(y_dtype=2), dict(h_dtype=3), dict(eps=0.0), dict(eps=float("inf")), dict(res_scale=float("nan")),
                dict(mod_stride=128), dict(mod_stride=258), dict(mod_stride=-256), dict(h_dtype=2), dict(post=0)):
         assert call(sh) == BAD, sh
-    assert call(dict(hidden=8200, mod_stride=8200)) == UNSUP
+    assert call(dict(hidden=8200, mod_stride=8200)) == UNSUP and call(dict(rows=(1 << 25) + 1)) == UNSUP
     for kw in (dict(x=None), dict(y=None), dict(x_out=None), dict(shift=None), dict(scale=None), dict(h=None), dict(h_scale=P),
                dict(x=P + 8), dict(y=P + 8), dict(gate=P + 4), dict(w_pre=P + 4), dict(row_batch=P + 2), dict(h=P + 2)):
         assert call(**kw) == BAD, kw

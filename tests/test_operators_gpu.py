@@ -261,6 +261,23 @@ def test_attention_offsets_beyond_32_bits():
     f.check()
 
 
+@pytest.mark.parametrize("dtype,H,nq", [("bf16", 16, 1100), ("bf16", 2, 3), ("f32", 2, 3)])
+def test_attention_bias_at_places_beyond_24_bits(dtype, H, nq):
+    """The distance of a near key is exact, however far down the cache the query stands (slopes that leave
+    keys more than 200 places away nothing)."""
+    dh, n, near = 64, 2 ** 24 + 1001, nq + 300
+    k, v = (torch.zeros(n, 1, dh, dtype=DT[dtype], device="cuda") for _ in range(2))
+    k[-near:], v[-near:] = rand(1, near, 1, dh, dtype=DT[dtype]), rand(2, near, 1, dh, dtype=DT[dtype])
+    q = rand(3, nq, H, dh, dtype=DT[dtype])
+    o = torch.empty_like(q)
+    slopes = np.linspace(1.0, 2.0, H)
+    s = dm.attn_shape(q, k, v, o, docs=1, max_q=nq, max_k=n, mask="causal")
+    dm.attention(s, q, k, v, o, dm.attention_workspace(s), slopes=torch.tensor(slopes, dtype=torch.float32, device="cuda"))
+    want, tol = ref_attention(np64(q), np64(k[-near:]), np64(v[-near:]), np.float64(np.float32(dh ** -0.5)), "causal",
+                              slopes=slopes.astype(np.float32).astype(np.float64), dtype=dtype)
+    close(np64(o), want, tol, "near keys")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_cuts_what_is_out_of_range(dtype):
     """Index arrays that leave the tensors are cut to them (the library cannot
@@ -274,6 +291,11 @@ def test_attention_cuts_what_is_out_of_range(dtype):
     a.o.fill_(7.0)
     a.run(q_start=i32([50, 40, 30]))  # no document has a row
     assert (a.o == 7.0).all()
+    a.run(q_start=i32([50, -2 ** 31, 2 ** 31 - 1]), k_start=i32([50, -2 ** 31, 2 ** 31 - 1]))
+    # the first has no row; the second is all rows, cut to max_q and max_k
+    want, tol = ref_attention(np64(a.q[:40]), np64(a.k[:40]), np64(a.v[:40]), np.float64(np.float32(64 ** -0.5)), dtype=dtype)
+    close(np64(a.o)[:40], want, tol, "all rows")
+    assert (a.o[40:] == 7.0).all()
     b = Attn(dtype, 2, 2, 64, [40], [40], seed=4)
     b.shape = dm.attn_shape(b.q, b.k, b.v, b.o, docs=1, max_q=16, max_k=20)
     b.ws = dm.attention_workspace(b.shape)
