@@ -99,6 +99,7 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f8_tile_kernel(LinF8Args 
   constexpr int IPW = (BM + BN) / (8 * NW);  // 1 KB DMA instructions per wave and block of k
   constexpr int STAGE = (BM + BN) * 128;  // W rows, then A rows
   constexpr int SC = BM * 32;             // scales of BM rows x 8 blocks
+  constexpr int PAIRS = (IPW + 1) / 2;
   static_assert(TN % 2 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && BM / 64 <= NW && 128 % (BN / WN) == 0, "tile split");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE + 2 * SC];
   float(*amax_s)[BM] = (float(*)[BM])smem;  // [WN][BM], after the last block
@@ -229,9 +230,9 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f8_tile_kernel(LinF8Args 
       // products: spread further they arrive late (up to 6% slower), right
       // behind the barrier they hold up the reads there (16% slower).  After the
       // last block: not read
-      if (x < IPW / 2) {
+      if (x < PAIRS) {
         issue_one(kb + 1, ~b & 1, 2 * x);
-        issue_one(kb + 1, ~b & 1, 2 * x + 1);
+        if (2 * x + 1 < IPW) issue_one(kb + 1, ~b & 1, 2 * x + 1);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -457,16 +458,18 @@ __global__ __launch_bounds__(256) void linear_f8_finish_kernel(LinF8Args a) {
 }
 
 // The plan of a product: at most 64 rows go to the kernel of few rows; else
-// tiles of 256 x 256 (one workgroup per CU; not for fp32 outputs, whose widened
-// operands need the registers) or 128 x 128 (two per CU), the last round's tiles
-// divided over k into up to eight ranges, by the least estimate of
-//   11 us a round + 1.85 us a block of k for 256 large tiles,
-//   4 us a round + 1.3 us a block for up to 512 small ones (0.7 us for up to 256),
-//   6 us (small tiles) or 10 us for adding ranges up
-// (measured at 1024 .. 17550 rows: 8192 x 1152 x 4608 73 us in small tiles, 83 in
-// large ones; 16384 x 8192 x 4096 645 and 515.  Ranges of two blocks did not pay:
-// 1024 x 1152 x 1152 23 us in four ranges, 10.1 us whole; 1024 x 4608 x 1152 25
-// against 32).
+// tiles of 256 x 256 or 192 x 256 (one workgroup per CU; not for fp32 outputs,
+// whose widened operands need the registers) or 128 x 128 (two per CU), the last
+// round's tiles divided over k into up to eight ranges, by the least estimate of
+//   `round` us for a round of up to `slots` tiles + `block` us for each of its
+//   blocks of k (`half` where it leaves half of the slots empty),
+//   `join` us for adding ranges up.
+// Measured at 1024 .. 17550 rows, in tiles of 128, 192 and 256:
+//   2048 x 1152 x 4608   27.7, 22.8, 27.9 us     8192 x 4608 x 1152  68, 54, 61
+//   6000 x 4096 x 4096   124, 101, 117           4352 x 3072 x 3072  63, 60, 49
+//   17550 x 12288 x 3072 904, 768, 724           1024 x 1152 x 4608  16, 19, 25
+// Ranges of two blocks did not pay: 1024 x 1152 x 1152 23 us in four ranges, 10.1
+// us whole; 1024 x 4608 x 1152 25 against 32.
 LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
   LinF8Plan p{};
   p.split = 1;
@@ -476,19 +479,23 @@ LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
   }
   const int KB = (K + 127) / 128;
   double best = 0;
-  for (int tile = 128; tile <= (dtype != 0 ? 256 : 128); tile *= 2) {
-    const long t = (long)((M + tile - 1) / tile) * ((N + tile - 1) / tile), slots = tile == 256 ? 256 : 512;
-    const long full = t / slots, rem = t % slots;
-    for (int s = 1; s <= 8 && (s == 1 || (KB >= 4 * s && rem * s <= slots && rem > 0)); ++s) {
-      const double round = tile == 256 ? 11 : 4, block = tile == 256 ? 1.85 : 1.3;
-      const double part = tile == 128 && rem * s <= 256 ? 0.7 : block;
-      const double us = full * (round + KB * block) + (rem ? round + KB * part / s + (s == 1 ? 0 : tile == 256 ? 10 : 6) : 0);
+  struct Tile {
+    int bm, bn, slots;
+    double round, block, half, join;
+  };
+  static const Tile tiles[3] = {{128, 128, 512, 4, 1.3, 0.7, 6}, {192, 256, 256, 9, 1.4, 1.4, 10}, {256, 256, 256, 11, 1.85, 1.85, 10}};
+  for (const Tile& c : tiles) {
+    if (dtype == 0 && c.bm != 128) break;
+    const long t = (long)((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), full = t / c.slots, rem = t % c.slots;
+    for (int s = 1; s <= 8 && (s == 1 || (KB >= 4 * s && rem * s <= c.slots && rem > 0)); ++s) {
+      const double part = rem * s <= 256 ? c.half : c.block;
+      const double us = full * (c.round + KB * c.block) + (rem ? c.round + KB * part / s + (s == 1 ? 0 : c.join) : 0);
       if (p.tile != 0 && us >= best) continue;
       best = us;
-      p.tile = tile;
+      p.tile = c.bm;
       p.split = s;
       p.n_full = (int)(s > 1 ? t - rem : t);
-      p.bytes = s > 1 ? (size_t)s * rem * tile * tile * 4 : 0;
+      p.bytes = s > 1 ? (size_t)s * rem * c.bm * c.bn * 4 : 0;
     }
   }
   return p;
@@ -525,6 +532,7 @@ static void launch_out(const LinF8Args& a, int tile, hipStream_t st) {
   }
   if constexpr (OUT != 0) {
     if (tile == 256) return launch_tile<256, 256, 4, 2, OUT>(a, st);
+    if (tile == 192) return launch_tile<192, 256, 4, 2, OUT>(a, st);
   }
   launch_tile<128, 128, 4, 2, OUT>(a, st);
 }

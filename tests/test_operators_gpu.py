@@ -360,7 +360,9 @@ LINEAR = [(1, 16, 1), (1, 1152, 6912), (3, 144, 40), (8, 1152, 136), (16, 4608, 
 LARGE = [(3990, 784, 4090, "gelu", "bf16"), (3990, 912, 4088, "none", "e4m3"), (4990, 2704, 4088, "gelu", "e4m3"),
          (4990, 2704, 4090, "none", "bf16"), (1900, 272, 4400, "gelu", "e4m3"), (1900, 272, 4400, "none", "bf16"), (1901, 128, 4501, "gelu", "bf16"),
          (4500, 1040, 4400, "none", "e4m3"), (4500, 1040, 4400, "gelu", "bf16"), (1900, 272, 4400, "none", "f32"),
-         (1030, 4608, 1160, "gelu", "f32"), (1030, 4608, 1160, "gelu", "e4m3")]
+         (1030, 4608, 1160, "gelu", "f32"), (1030, 4608, 1160, "gelu", "e4m3"),
+         (1343, 2320, 2970, "gelu", "bf16"), (1343, 2320, 2968, "none", "e4m3"),
+         (1547, 3184, 2473, "gelu", "bf16"), (1547, 3184, 2472, "gelu", "e4m3")]
 
 
 @pytest.mark.parametrize("M,K,N,act,dtype", [(*s, a, d) for s in LINEAR for a in ("none", "gelu") for d in ("bf16", "f32", "e4m3")] + LARGE)
