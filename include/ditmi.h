@@ -342,7 +342,7 @@ dit_status dit_quantize_fp8(int32_t rows, int32_t cols, int32_t block_rows, int3
  * fp32, otherwise on the 8-bit matrix pipe, which adds every 8 consecutive
  * products aligned to the largest of them with a last place of 2^-13 of its
  * binade, and those sums in fp32.
- *   rows >= 0, in a multiple of 16, out >= 1 (a multiple of 8 for DIT_E4M3)
+ *   rows >= 0, in a multiple of 16, out >= 1
  *   act    DIT_ACT_NONE, DIT_ACT_GELU (tanh)
  *   dtype  of out: DIT_F32, DIT_BF16, or DIT_E4M3, which quantises every row
  *          of y anew in blocks of 128 (as dit_quantize_fp8 with block_rows 1)

@@ -158,7 +158,7 @@ struct LinF8Args {
   // the first n_full tiles run whole; the k of each of the others is divided into `split` ranges of
   // whole blocks, whose fp32 partial tiles go to part[range][tile - n_full][rows][columns of a tile]
   int n_full, split;
-  float* part;  // (few rows with e4m3 outputs: fp32 sums [M][N])
+  float* part;  // (few rows with e4m3 outputs: fp32 sums [M][N rounded up to 4])
 };
 struct LinF8Plan {
   int tile;  // 0: the kernel of few rows; 128: tiles of 128 x 128; 192, 256: of so many rows x 256

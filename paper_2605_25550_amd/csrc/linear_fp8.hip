@@ -62,16 +62,17 @@ __device__ __forceinline__ float bias_at(const LinF8Args& a, int n) {
 template <int OUT>
 __device__ __forceinline__ void store_y4(const LinF8Args& a, bool whole, int m, int n, f32x4 y, float inv) {
   const long o = (long)m * a.N + n;
-  if (OUT == 2) {
-    *(uint32_t*)((uint8_t*)a.out + o) = pack_f8x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-  } else if (whole) {
-    if (OUT == 0) *(f32x4*)((float*)a.out + o) = y;
+  const uint32_t codes = OUT == 2 ? pack_f8x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv) : 0u;
+  if (whole) {
+    if (OUT == 2) *(uint32_t*)((uint8_t*)a.out + o) = codes;
+    else if (OUT == 0) *(f32x4*)((float*)a.out + o) = y;
     else *(u32x2*)((bf16_t*)a.out + o) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (n + e < a.N) {
-        if (OUT == 0) ((float*)a.out)[o + e] = y[e];
+        if (OUT == 2) ((uint8_t*)a.out)[o + e] = (uint8_t)(codes >> (8 * e));
+        else if (OUT == 0) ((float*)a.out)[o + e] = y[e];
         else ((bf16_t*)a.out)[o + e] = f2bf(y[e]);
       }
   }
@@ -283,7 +284,8 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f8_tile_kernel(LinF8Args 
       float mx = 0.f;
 #pragma unroll
       for (int j = 0; j < TN; ++j)
-        if (n0 + j * 16 + kq * 4 < a.N)  // N is a multiple of 8
+        // (columns past N repeat column N - 1, of the same block)
+        if (n0 + j * 16 + kq * 4 < a.N)
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fabsf(acc[j][i][e]));
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -322,7 +324,7 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f8_tile_kernel(LinF8Args 
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  if (OUT == 2 || a.N % 4 == 0) store_all(true);
+  if (a.N % 4 == 0) store_all(true);
   else store_all(false);
 }
 
@@ -347,6 +349,7 @@ __global__ __launch_bounds__(256) void linear_f8_reduce_kernel(LinF8Args a) {
     for (int e = 0; e < 4; ++e) {
       if (a.bias && n + e < a.N) y[e] += bias_at<OUT>(a, n + e);
       if (a.act) y[e] = gelu_tanh(y[e]);
+      if (OUT == 2 && n + e >= a.N) y[e] = 0.f;  // (no part of the block's maximum)
     }
   }
   if (OUT != 2) {
@@ -358,7 +361,7 @@ __global__ __launch_bounds__(256) void linear_f8_reduce_kernel(LinF8Args a) {
   mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
   const float sc = f8_scale(mx), inv = 1.0f / sc;
   if (!in) return;
-  store_y4<OUT>(a, true, m, n, y, inv);
+  store_y4<OUT>(a, a.N % 4 == 0, m, n, y, inv);
   if ((threadIdx.x & 31) == 0) a.out_scale[(long)m * ((a.N + 127) / 128) + n / 128] = sc;
 }
 
@@ -367,7 +370,8 @@ __global__ __launch_bounds__(256) void linear_f8_reduce_kernel(LinF8Args a) {
 // A workgroup owns 16 outputs of every row; its waves divide the blocks of k, with
 // the fragments of the next blocks loading from global memory while one is
 // multiplied, and add their sums through LDS in order.  e4m3, whose scales span
-// 128 outputs: fp32 sums go to part[M][N], and the finish kernel quantises them.
+// 128 outputs: fp32 sums go to part[M][part_row(N)], and the finish kernel quantises them.
+__host__ __device__ __forceinline__ int part_row(int N) { return (N + 3) & ~3; }  // of part: whole groups of four
 template <int TM, int NW, int OUT>
 __global__ __launch_bounds__(NW * 64) void linear_f8_rows_kernel(LinF8Args a) {
   constexpr bool WIDE = OUT == 0;
@@ -427,8 +431,8 @@ __global__ __launch_bounds__(NW * 64) void linear_f8_rows_kernel(LinF8Args a) {
     for (int w = 1; w < NW; ++w) y += sum[w][i][lane];
     const int m = i * 16 + r16, n = n0 + kq * 4;
     if (m >= a.M || n >= a.N) continue;
-    if (OUT == 2) {  // N is a multiple of 8
-      *(f32x4*)(a.part + (long)m * a.N + n) = y;
+    if (OUT == 2) {
+      *(f32x4*)(a.part + (long)m * part_row(a.N) + n) = y;
       continue;
     }
 #pragma unroll
@@ -447,11 +451,12 @@ __global__ __launch_bounds__(256) void linear_f8_finish_kernel(LinF8Args a) {
   const int m = bc / nb, n = (bc - m * nb) * 128 + (threadIdx.x & 31) * 4;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
   if (n < a.N) {
-    y = *(const f32x4*)(a.part + (long)m * a.N + n);
+    y = *(const f32x4*)(a.part + (long)m * part_row(a.N) + n);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (a.bias) y[e] += bias_at<2>(a, n + e);
+      if (a.bias && n + e < a.N) y[e] += bias_at<2>(a, n + e);
       if (a.act) y[e] = gelu_tanh(y[e]);
+      if (n + e >= a.N) y[e] = 0.f;
     }
   }
   float mx = fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3])));
@@ -459,7 +464,7 @@ __global__ __launch_bounds__(256) void linear_f8_finish_kernel(LinF8Args a) {
   mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
   const float sc = f8_scale(mx);
   if (blk >= a.M * nb) return;
-  if (n < a.N) store_y4<2>(a, true, m, n, y, 1.0f / sc);
+  if (n < a.N) store_y4<2>(a, a.N % 4 == 0, m, n, y, 1.0f / sc);
   if ((threadIdx.x & 31) == 0) a.out_scale[blk] = sc;
 }
 
@@ -480,7 +485,7 @@ LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
   LinF8Plan p{};
   p.split = 1;
   if (M <= 64) {
-    p.bytes = dtype == 2 ? (size_t)M * N * 4 : 0;
+    p.bytes = dtype == 2 ? (size_t)M * part_row(N) * 4 : 0;
     return p;
   }
   const int KB = (K + 127) / 128;

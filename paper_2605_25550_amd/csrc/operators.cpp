@@ -97,8 +97,6 @@ dit_status check_linear(const dit_linear_shape* s) {
   if (s->act != DIT_ACT_NONE && s->act != DIT_ACT_GELU) return fail(DIT_ERR_INVALID_ARG, "act %d unknown", s->act);
   if (s->dtype != DIT_F32 && s->dtype != DIT_BF16 && s->dtype != DIT_E4M3)
     return fail(DIT_ERR_INVALID_ARG, "dtype %d unknown", s->dtype);
-  if (s->dtype == DIT_E4M3 && s->out % 8 != 0)
-    return fail(DIT_ERR_INVALID_ARG, "out (%d) must be a multiple of 8 for 8-bit outputs", s->out);
   // 32-bit lane offsets of a tile's rows, tile counts of one grid dimension
   if ((long)s->in > (1L << 22) || (long)s->out > (1L << 26) || (long)s->rows > (1L << 26) ||
       (((long)s->rows + 31) / 32) * (((long)s->out + 31) / 32) >= (1L << 31))

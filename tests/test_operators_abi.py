@@ -97,7 +97,7 @@ def test_linear(dm):
     def call(M=4, K=256, N=128, act=0, dtype=1, a=P, sa=P, w=P, sw=P, bias=P, out=P, osc=None, ws=P, n=1 << 40):
         s = dm.LinearShape(M, K, N, act, dtype)
         return f(ctypes.byref(s), a, sa, w, sw, bias, out, osc, ws, n, None)
-    for kw in (dict(M=-1), dict(K=0), dict(K=24), dict(N=0), dict(act=2), dict(dtype=3), dict(dtype=2, N=20, osc=P), dict(dtype=2),
+    for kw in (dict(M=-1), dict(K=0), dict(K=24), dict(N=0), dict(act=2), dict(dtype=3), dict(dtype=2),
                dict(osc=P), dict(a=None), dict(a=P + 8), dict(sa=None), dict(w=None), dict(sw=None), dict(sw=P + 1), dict(bias=P + 2),
                dict(out=None), dict(dtype=2, osc=P + 1)):
         assert call(**kw) == BAD, kw
