@@ -785,11 +785,17 @@ hipError_t launch_doc_attn_merge(const DocAttnArgs& a, int head_dim, int dtype, 
 // bf16: up to 32 rows of a document and key head, and grids that its 32-row
 // workgroups do not fill (one for each CU; two of head_dim 64), go to the kernel
 // of few rows (one document of 256 tokens, 16 heads of 72: 8.5 us against 10.6).
-// A grid that leaves compute units idle divides the keys of its items into
-// ranges, of four tiles (256 keys; fp32: 128) at least, until there is a
-// workgroup for each unit (fp32, and few rows of 64: two).  More ranges cost more
-// in the merge than they gain (single tokens over 4 caches 17.8 us, 22 with
+// Of few rows, and in fp32, a grid that leaves compute units idle divides the keys
+// of its items into ranges, of four tiles (256 keys; fp32: 128) at least, until
+// there is a workgroup for each unit (fp32, and few rows of 64: two).  More ranges
+// cost more in the merge than they gain (single tokens over 4 caches 17.8 us, 22 with
 // twice as many).
+// 256-row workgroups divide where the least estimate says so: rounds of 256
+// workgroups (of a causal or prefix mask half the work, heaviest first, behind which
+// half an item ends) of 1.2 us a tile for head_dim 64, 1.5 for 72 and 128, and 10
+// us + 0.6 us per MB for partial results (7151 queries and keys, 12 heads on 4 of
+// 72: 280 us whole, 254 and 251 in two and three ranges; 881, 24 of 128: 30 and 37;
+// 3000, 16 of 64: 50 and 70; 4000 causal, 12 of 128: 86 and 110).
 DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype) {
   DocAttnPlan p{DOC_ROWS, 1};
   const long rows = (long)a.max_q * a.G;
@@ -798,9 +804,22 @@ DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype) {
   };
   const long fill = dtype == 1 && head_dim != 64 ? 256 : 512;
   if (dtype == 1 && (rows <= 32 || items(32) <= fill)) p.kernel = DOC_FEW;
-  const long n = items(p.kernel == DOC_FEW ? 32 : dtype == 1 ? 256 : 16);
-  const long want = dtype == 1 && p.kernel == DOC_ROWS ? 256 : fill;
-  if (n * 2 <= want) p.split = (int)std::max(1L, std::min({want / n, (long)a.max_k / (dtype == 1 ? 256 : 128), 32L}));
+  if (dtype != 1 || p.kernel == DOC_FEW) {
+    const long n = items(p.kernel == DOC_FEW ? 32 : 16);
+    if (n * 2 <= fill) p.split = (int)std::max(1L, std::min({fill / n, (long)a.max_k / (dtype == 1 ? 256 : 128), 32L}));
+    return p;
+  }
+  const long n = items(256);
+  const double T = (a.max_k + 63) / 64 * (head_dim == 64 ? 1.2 : 1.5);
+  const double mb = (double)std::min((long)a.docs * a.max_q, (long)a.q_rows) * a.H * (head_dim + 4) * 4e-6;
+  double best = 0;
+  for (int s = 1; s <= 8 && (s == 1 || a.max_k >= 256 * s); ++s) {
+    const double run = a.mask ? std::max(T / s, (n * T / 256 + T / s) / 2) : (double)((n * s + 255) / 256) / s * T;
+    const double us = run + (s > 1 ? 10 + 0.6 * mb * s : 0);
+    if (s > 1 && us >= best) continue;
+    best = us;
+    p.split = s;
+  }
   return p;
 }
 
