@@ -26,7 +26,7 @@
 // Bound by the matrix pipe and the vector instructions beside it (32 exponentials,
 // scalings, maxima and packs per lane and tile), which overlap in part: MFMA busy
 // 56% of the cycles at head_dim 128 (4352 queries and keys, 24 heads: 228 us, 1.02
-// PFLOP/s; two clips of 17550 keys: 1970 us, 1.17), 28% at head_dim 72, whose
+// PFLOP/s; clips of 12870 and 4680: 1970 us, 1.17), 28% at head_dim 72, whose
 // products pad to 80 and 96 columns (4 x 1024, 16 heads: 31.6 us, 0.61 PFLOP/s; a
 // slope of 1.5 us per tile and 8 us besides).  256 rows per workgroup, because
 // each row's share of the LDS reads of K and V falls with them; smaller
