@@ -4,7 +4,7 @@
 // fp32), the residual is updated, and the new row is normalised in turn.
 //
 // Bound by memory: 17550 x 3072 (bf16 y, e4m3 h) 121 us, 4.9 TB/s, the rate of a
-// plain copy on this card; 77 x 1152 3.6 us, a launch and a chain of loads.  A
+// plain copy on this card; 77 x 1152 4.7 us, a launch and a chain of loads.  A
 // wave owns a row (no barriers; its sums go through DPP), 4 columns per lane and chunk of 256, so that every fp32 access is 16
 // contiguous bytes per lane; where there are too few rows to fill the card with
 // waves, or a row is too wide for one wave's registers, a workgroup of four
