@@ -29,8 +29,8 @@
 // PFLOP/s; clips of 12870 and 4680: 1970 us, 1.17), 28% at head_dim 72, whose
 // products pad to 80 and 96 columns (4 x 1024, 16 heads: 31.6 us, 0.61 PFLOP/s; a
 // slope of 1.5 us per tile and 8 us besides).  256 rows per workgroup, because
-// each row's share of the LDS reads of K and V falls with them; smaller
-// workgroups, and key ranges for many rows, were slower.
+// each row's share of the LDS reads of K and V falls with them; four waves a
+// workgroup were slower, and key ranges pay in few grids only (doc_attn_plan).
 #include <algorithm>
 
 #include "common.h"
