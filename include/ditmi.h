@@ -284,8 +284,9 @@ dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, floa
  *   o = softmax over the visible keys of s, times v
  * A query without a visible key gets zeros.  What k and v hold in rows that a
  * query cannot see (NaN and infinities included) does not reach it.  A score
- * of -inf counts as not visible.  Rows of o outside every document are left
- * as they were.  fp32 softmax and sums; in bf16 the probabilities, taken
+ * of -inf gives its key the weight 0, and a query that has no other zeros (with
+ * a cap, an infinite q.k is a score of -cap or cap).  Rows of o outside every
+ * document are left as they were.  fp32 softmax and sums; in bf16 the probabilities, taken
  * relative to a running maximum, are rounded to bf16 before the product with
  * v, and their sum is that of the rounded ones.
  *   docs >= 1;  heads a multiple of kv_heads;  head_dim in {64, 72, 128}

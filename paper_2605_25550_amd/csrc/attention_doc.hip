@@ -418,16 +418,16 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
       }
     }
     m = max_halves(m);
-    // (of a row without a visible key here, the max stays -inf whatever the cap makes of it)
-    lead(m == -INFINITY ? m : score.z_of_max(m));
+    // The limit says what is visible, never the value: a raw score of -inf may be
+    // visible, and -cap.  (Of a row without a visible key here the max stays -inf.)
+    lead(kv0 < lim ? score.z_of_max(m) : -INFINITY);
     u32x4 pw[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const int e = (c & 1) * 8 + 2 * w;
-        const float x = s[c >> 1][e], y = s[c >> 1][e + 1];
-        pw[c][w] = pack_bf16x2(x == -INFINITY ? 0.f : prob(x), y == -INFINITY ? 0.f : prob(y));
+        const int e = (c & 1) * 8 + 2 * w, key = kv0 + (c >> 1) * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
+        pw[c][w] = pack_bf16x2(key < lim ? prob(s[c >> 1][e]) : 0.f, key + 1 < lim ? prob(s[c >> 1][e + 1]) : 0.f);
         if (w & 1) add_sum(pw[c][w - 1], pw[c][w]);
       }
     __syncthreads();  // V has been cleaned
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
         m = fmaxf(m, s[kt][e]);
       }
     m = max_halves(m);
-    m = m == -INFINITY ? m : score.z_of_max(m);
+    m = kv0 < lim ? score.z_of_max(m) : -INFINITY;
     const float m_new = fmaxf(m_run, m), mneg = m_new == -INFINITY ? 0.f : -m_new;
     const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
     l_run *= alpha;
@@ -617,9 +617,9 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const int e = (c & 1) * 8 + 2 * w;
-        const float x = s[c >> 1][e], y = s[c >> 1][e + 1];
-        pw[c][w] = pack_bf16x2(x == -INFINITY ? 0.f : score.prob(x, mneg), y == -INFINITY ? 0.f : score.prob(y, mneg));
+        // (the limit says what is visible, as above)
+        const int e = (c & 1) * 8 + 2 * w, key = kv0 + (c >> 1) * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
+        pw[c][w] = pack_bf16x2(key < lim ? score.prob(s[c >> 1][e], mneg) : 0.f, key + 1 < lim ? score.prob(s[c >> 1][e + 1], mneg) : 0.f);
         l_run += __uint_as_float(pw[c][w] << 16) + __uint_as_float(pw[c][w] & 0xFFFF0000u);
       }
     if (more) wait_vmcnt<C::KDMA>();  // this tile's V (the next K may be under way)

@@ -1,0 +1,41 @@
+"""Scores and values at the ends of their types, for each kernel of the
+masked attention, against the 64-bit definitions of operator_refs.py."""
+import pytest
+import torch
+
+from test_operators_gpu import Attn
+
+pytestmark = pytest.mark.gpu
+
+# (type, query heads, key heads, queries, keys, room) of a call that the kernel takes
+KERNELS = {"rows": ("bf16", 24, 24, [600, 333], [600, 333], 0),        # 256-row workgroups: whole and masked tiles
+           "ranges": ("bf16", 24, 3, [700, 5], [6000, 900], 6000),     # ... that divide the keys
+           "few": ("bf16", 4, 2, [150, 3], [150, 90], 200),            # 32-row workgroups
+           "tokens": ("bf16", 4, 2, [1, 2], [2000, 700], 2000),        # ... that divide the keys
+           "f32": ("f32", 6, 2, [150, 3], [150, 90], 200)}
+
+
+def call(kernel, dh, **kw):
+    dtype, H, Hk, ql, kl, room = KERNELS[kernel]
+    return Attn(dtype, H, Hk, dh, ql, kl, room=room, fused=False, seed=dh, **kw)
+
+
+@pytest.mark.parametrize("bias", [False, True], ids=["cap", "cap+bias"])
+@pytest.mark.parametrize("dh", [64, 72, 128])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_capped_scores_of_infinite_products(kernel, dh, bias):
+    """cap * tanh(-inf / cap) is -cap, a score like any other, wherever its key
+    lies: in tiles that every row sees whole, on the diagonal, in the last."""
+    a = call(kernel, dh, mask="causal", cap=1.0, bias=bias)
+    a.q[:, :, 0] = 1.0
+    a.k[:, :, 0] = 0.0
+    # the definition's infinities: tanh(-40) is -1 within 2^-113
+    far = float(torch.tensor(40 * dh ** 0.5, dtype=a.k.dtype))
+    finite = a.k.clone()
+    for d, n in enumerate(a.kl):
+        rows, fin = a.k[a.k0[d]:a.k0[d] + n], finite[a.k0[d]:a.k0[d] + n]
+        for at, sign in ((slice(0, 1), -1), (slice(3, None, 7), -1), (slice(5, None, 31), 1), (slice(n - 1, n), -1)):
+            rows[at, :, 0], fin[at, :, 0] = sign * float("inf"), sign * far
+    a.run()
+    a.k = finite
+    a.check()
