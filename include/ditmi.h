@@ -288,7 +288,10 @@ dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, floa
  * a cap, an infinite q.k is a score of -cap or cap).  Rows of o outside every
  * document are left as they were.  fp32 softmax and sums; in bf16 the probabilities, taken
  * relative to a running maximum, are rounded to bf16 before the product with
- * v, and their sum is that of the rounded ones.
+ * v, and their sum is that of the rounded ones.  No probability exceeds 1, and
+ * they are added up before the division by their sum: finite values of v give
+ * finite results as long as the largest times the number of visible keys stays
+ * below 2^127.
  *   docs >= 1;  heads a multiple of kv_heads;  head_dim in {64, 72, 128}
  *   q_rows, k_rows   rows of q and o, rows of k and v (every room counted)
  *   max_q, max_k     no document has more query rows, or keys (longer ones

@@ -39,3 +39,20 @@ def test_capped_scores_of_infinite_products(kernel, dh, bias):
     a.run()
     a.k = finite
     a.check()
+
+
+@pytest.mark.parametrize("rise", [15, 40, 63])
+@pytest.mark.parametrize("dh", [64, 72, 128])
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_large_values_under_rising_scores(kernel, dh, rise):
+    """Scores that rise by a factor of 2^rise from tile to tile, values of some
+    2^100: their number times the largest is below 2^127, so that every result is
+    finite, whichever maximum the probabilities are taken relative to."""
+    a = call(kernel, dh, mask="causal")
+    a.q[:, :, 0] = 1.0
+    for d, n in enumerate(a.kl):
+        a.k[a.k0[d]:a.k0[d] + n, :, 0] = (torch.arange(n, device="cuda") // 64 * (rise * dh ** 0.5 / 1.4427))[:, None]
+    a.v.mul_(2.0 ** 100)
+    a.run()
+    assert a.o.isfinite().all()
+    a.check()
