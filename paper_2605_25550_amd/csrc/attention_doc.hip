@@ -423,15 +423,18 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
     }
     m = max_halves(m);
     // The limit says what is visible, never the value: a raw score of -inf may be
-    // visible, and -cap.  (Of a row without a visible key here the max stays -inf.)
+    // visible, and -cap.  (Of a row without a visible key here the max stays -inf;
+    // without a raw score to be capped, 2^-inf is the 0 of what is not visible.)
     lead(kv0 < lim ? score.z_of_max(m) : -INFINITY);
+    const int seen = lim - kv0 - g * 4;
+    auto seen_prob = [&](float x, int off) { return !CAP || BIAS || off < seen ? prob(x) : 0.f; };
     u32x4 pw[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const int e = (c & 1) * 8 + 2 * w, key = kv0 + (c >> 1) * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
-        pw[c][w] = pack_bf16x2(key < lim ? prob(s[c >> 1][e]) : 0.f, key + 1 < lim ? prob(s[c >> 1][e + 1]) : 0.f);
+        const int e = (c & 1) * 8 + 2 * w, off = (c >> 1) * 32 + (e >> 2) * 8 + (e & 3);
+        pw[c][w] = pack_bf16x2(seen_prob(s[c >> 1][e], off), seen_prob(s[c >> 1][e + 1], off + 1));
         if (w & 1) add_sum(pw[c][w - 1], pw[c][w]);
       }
     __syncthreads();  // V has been cleaned
@@ -611,6 +614,8 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     m = max_halves(m);
     m = kv0 < lim ? score.z_of_max(m) : -INFINITY;
     const float m_new = fmaxf(m_run, m), mneg = m_new == -INFINITY ? 0.f : -m_new;
+    const int seen = lim - kv0 - g * 4;  // (the limit says what is visible, as above)
+    auto seen_prob = [&](float x, int off) { return !CAP || BIAS || off < seen ? score.prob(x, mneg) : 0.f; };
     const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
     l_run *= alpha;
 #pragma unroll
@@ -621,9 +626,8 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        // (the limit says what is visible, as above)
-        const int e = (c & 1) * 8 + 2 * w, key = kv0 + (c >> 1) * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
-        pw[c][w] = pack_bf16x2(key < lim ? score.prob(s[c >> 1][e], mneg) : 0.f, key + 1 < lim ? score.prob(s[c >> 1][e + 1], mneg) : 0.f);
+        const int e = (c & 1) * 8 + 2 * w, off = (c >> 1) * 32 + (e >> 2) * 8 + (e & 3);
+        pw[c][w] = pack_bf16x2(seen_prob(s[c >> 1][e], off), seen_prob(s[c >> 1][e + 1], off + 1));
         l_run += __uint_as_float(pw[c][w] << 16) + __uint_as_float(pw[c][w] & 0xFFFF0000u);
       }
     if (more) wait_vmcnt<C::KDMA>();  // this tile's V (the next K may be under way)
