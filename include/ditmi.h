@@ -301,7 +301,8 @@ dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, floa
  *   *_row, *_head    strides in elements between rows and between heads of
  *                    each tensor, multiples of 8 (bf16) or 4 (fp32); the
  *                    head_dim elements of a head are contiguous.  Rows at
- *                    most 2^22 elements apart. */
+ *                    most 2^22 elements apart.  No two pieces (row, head) of
+ *                    o may share elements. */
 typedef enum { DIT_MASK_FULL = 0, DIT_MASK_CAUSAL = 1, DIT_MASK_PREFIX = 2 } dit_attn_mask;
 typedef struct {
   int32_t docs, heads, kv_heads, head_dim;
@@ -315,8 +316,10 @@ typedef struct {
  * to size_t for an invalid shape, dit_last_error() then says why. */
 size_t dit_attention_workspace_bytes(const dit_attn_shape *s);
 
-/*   q_start, k_start  [docs + 1] int32, or NULL for equal rooms of max_q
- *                     query rows (max_k key rows) each
+/*   q_start, k_start  [docs + 1] int32, not falling, or NULL for equal rooms of
+ *                     max_q query rows (max_k key rows) each.  (Of a q_start
+ *                     that falls, documents may share query rows; each such row
+ *                     of o then holds pieces of their results.)
  *   k_len             [docs] int32 filled keys of each document, or NULL: all
  *   prefix            [docs] int32 (DIT_MASK_PREFIX; NULL otherwise)
  *   slopes            [heads] fp32, or NULL

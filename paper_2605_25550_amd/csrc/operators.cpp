@@ -26,6 +26,16 @@ dit_status check_strides(const char* name, int64_t row, int64_t head, int heads,
   return DIT_OK;
 }
 
+// Whether two of o's dh-element pieces (row, head) share elements: dr rows and h heads
+// apart they lie |dr row - h head| elements apart (or the sum, which is larger).
+bool pieces_overlap(int64_t row, int64_t head, int64_t rows, int64_t heads, int64_t dh) {
+  if (rows < 2 || heads < 2 || row >= (heads - 1) * head + dh || head >= (rows - 1) * row + dh) return false;
+  for (int64_t h = 1; h < heads; ++h)
+    for (int64_t dr = h * head / row; dr <= h * head / row + 1 && dr < rows; ++dr)
+      if (dr * row - h * head < dh && h * head - dr * row < dh) return true;
+  return false;
+}
+
 dit_status check_attn(const dit_attn_shape* s) {
   if (!s) return fail(DIT_ERR_INVALID_ARG, "shape is NULL");
   if (s->docs < 1 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads != 0)
@@ -55,7 +65,11 @@ dit_status check_attn(const dit_attn_shape* s) {
   if ((st = check_strides("q", s->q_row, s->q_head, s->heads, s->q_rows, dh, unit)) != DIT_OK) return st;
   if ((st = check_strides("k", s->k_row, s->k_head, s->kv_heads, s->k_rows, dh, unit)) != DIT_OK) return st;
   if ((st = check_strides("v", s->v_row, s->v_head, s->kv_heads, s->k_rows, dh, unit)) != DIT_OK) return st;
-  return check_strides("o", s->o_row, s->o_head, s->heads, s->q_rows, dh, unit);
+  if ((st = check_strides("o", s->o_row, s->o_head, s->heads, s->q_rows, dh, unit)) != DIT_OK) return st;
+  if (pieces_overlap(s->o_row, s->o_head, s->q_rows, s->heads, dh))
+    return fail(DIT_ERR_INVALID_ARG, "o strides (%lld, %lld): rows and heads of %d elements overlap", (long long)s->o_row,
+                (long long)s->o_head, dh);
+  return DIT_OK;
 }
 
 DocAttnArgs attn_args(const dit_attn_shape* s) {

@@ -71,6 +71,23 @@ def test_attention_pointers_and_workspace(dm):
     assert call_attn(dm, big, ws=None) == BAD and call_attn(dm, big, ws=P + 16) == BAD
 
 
+@pytest.mark.parametrize("row,head,rows,ok", [
+    (512, 64, 100, True), (64, 6400, 100, True), (1024, 128, 100, True),      # by row, by head, with gaps
+    (128, 64 + 128 * 100, 100, True), (448, 64, 1, True), (64, 128, 2, True),  # ... one row, rows between the heads
+    (1088, 256, 100, True),                                                    # 4 head strides are a row less a piece
+    (64, 64, 100, False), (128, 64, 100, False), (504, 64, 100, False), (448, 64, 2, False), (64, 6336, 100, False),
+    (64, 192, 4, False), (1024, 256, 100, False), (1032, 256, 100, False), (1016, 256, 100, False)])
+def test_attention_pieces_of_o_do_not_overlap(dm, row, head, rows, ok):
+    s = attn(dm, o_row=row, o_head=head, q_rows=rows)
+    at = {(r, h): r * row + h * head for r in range(rows) for h in range(8)}
+    starts = sorted(at.values())
+    assert ok == all(b - a >= 64 for a, b in zip(starts, starts[1:]))
+    bad = dm.lib().dit_attention_workspace_bytes(s) == ctypes.c_size_t(-1).value
+    assert bad != ok
+    if not ok:
+        assert call_attn(dm, s) == BAD and "o strides" in dm.last_error()
+
+
 def test_attention_of_no_rows(dm):
     """Nothing to do is no error, and needs no tensors."""
     s = attn(dm, q_rows=0, max_q=0)
