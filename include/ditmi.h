@@ -379,7 +379,8 @@ dit_status dit_linear_fp8(const dit_linear_shape *s, const void *a, const float 
  * DIT_NORM_LAYER subtracts the mean and divides by the standard deviation
  * (biased variance), DIT_NORM_RMS divides by the root mean square, both with
  * eps; DIT_NORM_NONE (post only) leaves y as it is.  b = row_batch[row].
- *   rows >= 0 (at most 2^25), hidden a multiple of 8 in 8 .. 8192
+ *   rows >= 0 (at most 2^25; 2^24 - 1 of more than 4096 columns), hidden a
+ *              multiple of 8 in 8 .. 8192
  *   batch      rows of gate, shift and scale, mod_stride elements apart (a
  *              multiple of 4): slices of one modulation matrix
  *   y_dtype    of y: DIT_F32 or DIT_BF16

@@ -269,8 +269,10 @@ dit_status dit_norm_residual(const dit_norm_shape* s, const float* x, float* x_o
   if (s->rows < 0 || s->hidden < 8 || s->hidden % 8 != 0 || s->batch < 1)
     return fail(DIT_ERR_INVALID_ARG, "rows (%d) must be >= 0, hidden (%d) a positive multiple of 8, batch (%d) >= 1",
                 s->rows, s->hidden, s->batch);
-  if (s->hidden > 8192 || s->rows > (1 << 25))  // (a grid has fewer than 2^32 threads: 64 for a row)
-    return fail(DIT_ERR_UNSUPPORTED, "%d rows of %d: more than 2^25 rows or 8192 columns are not supported", s->rows, s->hidden);
+  // (a grid has fewer than 2^32 threads: 64 for a row, 256 from 4097 columns on)
+  if (s->hidden > 8192 || s->rows > (s->hidden > 4096 ? (1 << 24) - 1 : 1 << 25))
+    return fail(DIT_ERR_UNSUPPORTED, "%d rows of %d: at most 8192 columns, and 2^25 rows (2^24 - 1 of more than 4096)",
+                s->rows, s->hidden);
   if (s->post < DIT_NORM_NONE || s->post > DIT_NORM_RMS || s->pre < DIT_NORM_LAYER || s->pre > DIT_NORM_RMS)
     return fail(DIT_ERR_INVALID_ARG, "norms (post %d, pre %d) unknown", s->post, s->pre);
   if ((s->y_dtype != DIT_F32 && s->y_dtype != DIT_BF16) || s->h_dtype < DIT_F32 || s->h_dtype > DIT_E4M3)

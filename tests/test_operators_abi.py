@@ -154,6 +154,17 @@ def test_norm(dm):
     assert call(dict(rows=0), x=None, row_batch=None) == 0
 
 
+@pytest.mark.parametrize("hidden,rows,ok", [(4096, 1 << 25, True), (4096, (1 << 25) + 1, False), (4104, (1 << 24) - 1, True),
+                                            (4104, 1 << 24, False), (8192, 1 << 24, False), (8192, 1 << 25, False)])
+def test_norm_grid(dm, hidden, rows, ok):
+    """Rows of more than 4096 columns take 256 threads each, and a grid has fewer than 2^32.  (What passes is refused
+    by the next check, for its pointer.)"""
+    s = dm.NormShape(rows, hidden, 1, 0, 1, 0, 1, 1e-6, 1.0, hidden)
+    got = dm.lib().dit_norm_residual(ctypes.byref(s), None, None, None, None, None, None, None, None, None, P, None, None)
+    assert got == (BAD if ok else UNSUP), dm.last_error()
+    assert not ok or "x NULL" in dm.last_error()
+
+
 def test_binding_refuses_host_tensors_wrong_types_and_sizes(dm):
     t = torch.zeros(4, 2, 64)
     with pytest.raises(ValueError):  # mixed types
