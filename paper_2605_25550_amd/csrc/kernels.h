@@ -161,7 +161,7 @@ struct LinF8Args {
   float* part;  // (few rows with e4m3 outputs: fp32 sums [M][N rounded up to 4])
 };
 struct LinF8Plan {
-  int tile;  // 0: the kernel of few rows; 128: tiles of 128 x 128; 192, 256: of so many rows x 256
+  int tile;  // 0: the kernel of few rows; 128: tiles of 128 x 128; 192, 256: of so many rows x 256; -1: it would take a grid of 2^32 threads
   int n_full, split;
   size_t bytes;  // of part
 };

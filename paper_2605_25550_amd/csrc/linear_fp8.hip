@@ -481,14 +481,21 @@ __global__ __launch_bounds__(256) void linear_f8_finish_kernel(LinF8Args a) {
 //   17550 x 12288 x 3072 904, 768, 724           1024 x 1152 x 4608  16, 19, 25
 // Ranges of two blocks did not pay: 1024 x 1152 x 1152 23 us in four ranges, 10.1
 // us whole; 1024 x 4608 x 1152 25 against 32.
+static constexpr long MAX_THREADS = 1L << 32;  // a grid has fewer
+// Waves of a workgroup of the kernel of few rows: at least two blocks of k for each;
+// sixteen have the registers of up to 32 rows.
+static int rows_waves(int M, int KB) { return KB < 16 ? 4 : KB < 32 || M > 32 ? 8 : 16; }
+
 LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
   LinF8Plan p{};
   p.split = 1;
+  const int KB = (K + 127) / 128;
   if (M <= 64) {
+    if ((long)((N + 15) / 16) * rows_waves(M, KB) * 64 >= MAX_THREADS) p.tile = -1;
     p.bytes = dtype == 2 ? (size_t)M * part_row(N) * 4 : 0;
     return p;
   }
-  const int KB = (K + 127) / 128;
+  p.tile = -1;
   double best = 0;
   struct Tile {
     int bm, bn, slots;
@@ -501,7 +508,7 @@ LinF8Plan linear_fp8_plan(int M, int N, int K, int dtype) {
     for (int s = 1; s <= 8 && (s == 1 || (KB >= 4 * s && rem * s <= c.slots && rem > 0)); ++s) {
       const double part = rem * s <= 256 ? c.half : c.block;
       const double us = full * (c.round + KB * c.block) + (rem ? c.round + KB * part / s + (s == 1 ? 0 : c.join) : 0);
-      if (p.tile != 0 && us >= best) continue;
+      if ((t + c.slots) * 512 >= MAX_THREADS || (p.tile > 0 && us >= best)) continue;
       best = us;
       p.tile = c.bm;
       p.split = s;
@@ -522,12 +529,10 @@ static void launch_tile(const LinF8Args& a, hipStream_t st) {
 
 template <int TM, int OUT>
 static void launch_rows(const LinF8Args& a, hipStream_t st) {
-  const int KB = (a.K + 127) / 128;
   const dim3 grid((a.N + 15) / 16);
-  // at least two blocks of k for each wave; sixteen waves have the registers of
-  // up to 32 rows
-  if (KB < 16) hipLaunchKernelGGL((linear_f8_rows_kernel<TM, 4, OUT>), grid, dim3(256), 0, st, a);
-  else if (KB < 32 || TM == 4) hipLaunchKernelGGL((linear_f8_rows_kernel<TM, 8, OUT>), grid, dim3(512), 0, st, a);
+  const int nw = rows_waves(a.M, (a.K + 127) / 128);
+  if (nw == 4) hipLaunchKernelGGL((linear_f8_rows_kernel<TM, 4, OUT>), grid, dim3(256), 0, st, a);
+  else if (nw == 8) hipLaunchKernelGGL((linear_f8_rows_kernel<TM, 8, OUT>), grid, dim3(512), 0, st, a);
   else hipLaunchKernelGGL((linear_f8_rows_kernel<TM == 4 ? 2 : TM, 16, OUT>), grid, dim3(1024), 0, st, a);
   if (OUT == 2)
     hipLaunchKernelGGL(linear_f8_finish_kernel, dim3((a.M * ((a.N + 127) / 128) + 7) / 8), dim3(256), 0, st, a);

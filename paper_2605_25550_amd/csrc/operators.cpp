@@ -103,6 +103,10 @@ size_t attn_bytes(const dit_attn_shape* s, const DocAttnPlan& p) {
 }
 
 // ------------------------------------------------------------------ linear
+LinF8Plan plan_linear(const dit_linear_shape* s) {
+  return s->rows > 0 ? linear_fp8_plan(s->rows, s->out, s->in, s->dtype) : LinF8Plan{};
+}
+
 dit_status check_linear(const dit_linear_shape* s) {
   if (!s) return fail(DIT_ERR_INVALID_ARG, "shape is NULL");
   if (s->rows < 0 || s->in < 16 || s->in % 16 != 0 || s->out < 1)
@@ -113,12 +117,9 @@ dit_status check_linear(const dit_linear_shape* s) {
     return fail(DIT_ERR_INVALID_ARG, "dtype %d unknown", s->dtype);
   // 32-bit lane offsets of a tile's rows, tile counts of one grid dimension
   if ((long)s->in > (1L << 22) || (long)s->out > (1L << 26) || (long)s->rows > (1L << 26) ||
-      (((long)s->rows + 31) / 32) * (((long)s->out + 31) / 32) >= (1L << 31))
+      (((long)s->rows + 31) / 32) * (((long)s->out + 31) / 32) >= (1L << 31) || plan_linear(s).tile < 0)
     return fail(DIT_ERR_UNSUPPORTED, "product of %d x %d x %d is too large", s->rows, s->out, s->in);
   return DIT_OK;
-}
-size_t linear_bytes(const dit_linear_shape* s) {
-  return s->rows > 0 ? linear_fp8_plan(s->rows, s->out, s->in, s->dtype).bytes : 0;
 }
 
 dit_status check_ws(const void* ws, size_t bytes, size_t need) {
@@ -221,7 +222,7 @@ dit_status dit_quantize_fp8(int32_t rows, int32_t cols, int32_t block_rows, int3
 
 size_t dit_linear_fp8_workspace_bytes(const dit_linear_shape* s) {
   if (check_linear(s) != DIT_OK) return BAD_SIZE;
-  return linear_bytes(s);
+  return plan_linear(s).bytes;
 }
 
 dit_status dit_linear_fp8(const dit_linear_shape* s, const void* a, const float* a_scale, const void* w,
@@ -237,7 +238,8 @@ dit_status dit_linear_fp8(const dit_linear_shape* s, const void* a, const float*
   TRY(check_ptr(bias, "bias", 16, true));
   TRY(check_ptr(out, "out", 16, false));
   TRY(check_ptr(out_scale, "out_scale", 4, s->dtype != DIT_E4M3));
-  TRY(check_ws(workspace, ws_bytes, linear_bytes(s)));
+  const LinF8Plan p = plan_linear(s);
+  TRY(check_ws(workspace, ws_bytes, p.bytes));
   LinF8Args l{};
   l.a = (const uint8_t*)a;
   l.w = (const uint8_t*)w;
@@ -251,7 +253,6 @@ dit_status dit_linear_fp8(const dit_linear_shape* s, const void* a, const float*
   l.K = s->in;
   l.act = s->act;
   l.dtype = s->dtype;
-  const LinF8Plan p = linear_fp8_plan(l.M, l.N, l.K, l.dtype);
   l.n_full = p.n_full;
   l.split = p.split;
   l.part = (float*)workspace;

@@ -165,6 +165,20 @@ def test_norm_grid(dm, hidden, rows, ok):
     assert not ok or "x NULL" in dm.last_error()
 
 
+@pytest.mark.parametrize("M,K,N,dtype,ok", [
+    (1, 4096, (1 << 26) - 16, 1, True), (1, 4096, (1 << 26) - 15, 1, False), (32, 4096, 1 << 26, 0, False),
+    (33, 4096, 1 << 26, 1, True), (1, 128, 1 << 26, 2, True),                       # 1024, 512 and 256 threads for 16 columns
+    (1 << 20, 128, (1 << 17) - 128, 0, True), (1 << 20, 128, 1 << 17, 0, False),    # fp32 has tiles of 128 x 128 alone
+    (1 << 20, 128, 1 << 17, 2, True), (1 << 20, 128, 1 << 19, 2, False)])           # the others larger ones
+def test_linear_grids(dm, M, K, N, dtype, ok):
+    """No call that passes the checks asks for a grid of 2^32 threads."""
+    s = dm.LinearShape(M, K, N, 0, dtype)
+    got = dm.lib().dit_linear_fp8(ctypes.byref(s), None, P, P, P, None, P, P if dtype == 2 else None, None, 0, None)
+    assert got == (BAD if ok else UNSUP), dm.last_error()
+    assert not ok or "a NULL" in dm.last_error()
+    assert ok != (dm.lib().dit_linear_fp8_workspace_bytes(s) == ctypes.c_size_t(-1).value)
+
+
 def test_binding_refuses_host_tensors_wrong_types_and_sizes(dm):
     t = torch.zeros(4, 2, 64)
     with pytest.raises(ValueError):  # mixed types
