@@ -821,7 +821,9 @@ DocAttnPlan doc_attn_plan(const DocAttnArgs& a, int head_dim, int dtype) {
   const double T = (a.max_k + 63) / 64 * (head_dim == 64 ? 1.2 : 1.5);
   const double mb = (double)std::min((long)a.docs * a.max_q, (long)a.q_rows) * a.H * (head_dim + 4) * 4e-6;
   double best = 0;
-  for (int s = 1; s <= 8 && (s == 1 || a.max_k >= 256 * s); ++s) {
+  // (the merge pass takes a thread for four columns of a query and head, of fewer than 2^32 in a grid)
+  const bool merges = (long)a.max_q * a.H * (head_dim / 4) < (1L << 32) - 256;
+  for (int s = 1; s <= 8 && (s == 1 || (merges && a.max_k >= 256 * s)); ++s) {
     const double run = a.mask ? std::max(T / s, (n * T / 256 + T / s) / 2) : (double)((n * s + 255) / 256) / s * T;
     const double us = run + (s > 1 ? 10 + 0.6 * mb * s : 0);
     if (s > 1 && us >= best) continue;

@@ -88,6 +88,16 @@ def test_attention_pieces_of_o_do_not_overlap(dm, row, head, rows, ok):
         assert call_attn(dm, s) == BAD and "o strides" in dm.last_error()
 
 
+@pytest.mark.parametrize("max_q", [(1 << 27) // 33, (1 << 27) // 31])
+def test_attention_merge_grid(dm, max_q):
+    """Rows divide their keys only where the merge pass, a thread for four columns, has fewer than 2^32 threads."""
+    s = attn(dm, docs=1, heads=32, kv_heads=16, head_dim=128, q_rows=max_q, max_q=max_q, k_rows=1 << 29, max_k=1 << 29, mask=1,
+             q_row=4096, q_head=128, k_row=2048, k_head=128, v_row=2048, v_head=128, o_row=4096, o_head=128)
+    need = dm.lib().dit_attention_workspace_bytes(s)
+    assert need != ctypes.c_size_t(-1).value
+    assert (need > 0) == (max_q * 32 * 32 < 1 << 32)
+
+
 def test_attention_of_no_rows(dm):
     """Nothing to do is no error, and needs no tensors."""
     s = attn(dm, q_rows=0, max_q=0)
