@@ -71,6 +71,7 @@ struct DocCfg {
     return c ^ (DHP == 128 ? (r & 3) << 2 : (DHP == 64 ? ((r >> 1) & 1) << 2 : 0));
   }
   static_assert(TILE % 1024 == 0 && VTILE % 1024 == 0 && ST * VTILE <= 65536, "whole DMA blocks; slot offsets fit the LDS immediate");
+  static_assert(DT * 64 <= VROW, "transposed reads stay in their rows");
 };
 
 // Holds a value's computation where it is written: the compiler orders pure
@@ -147,8 +148,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
   constexpr int NDMA = C::KDMA + C::VDMA, IPW = (NDMA + NW - 1) / NW;  // DMA instructions per wave and tile (uniform)
   constexpr bool SPARE = IPW * NW > NDMA;
   constexpr int VBASE = ST * C::TILE, SPARE_AT = VBASE + ST * C::VTILE;
-  // the ring, then a line that absorbs spare DMAs (and what transposed reads of
-  // head_dim 72 touch past the last V row)
+  // the ring, then a line that absorbs spare DMAs
   __shared__ __attribute__((aligned(1024))) unsigned char smem[ST * (C::TILE + C::VTILE) + 1024];
   __shared__ int bad[3][DH];
 
@@ -224,8 +224,6 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
       dma_16s(base, o, dst);
   };
   for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
-  if (C::FOLD)
-    for (int e = tid; e < 256; e += NW * 64) ((uint32_t*)(smem + SPARE_AT))[e] = 0;
 
   const lds_byte* k_at[C::KS];
 #pragma unroll
@@ -505,7 +503,7 @@ template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   using C = DocCfg<DH>;
   constexpr int NW = 4, OS = DH + 4;
-  constexpr int RING = C::TILE + C::VTILE + 256;  // of one wave (+ what transposed reads of head_dim 72 touch past V)
+  constexpr int RING = C::TILE + C::VTILE;  // of one wave
   static_assert(NW * RING >= NW * 32 * OS * 4, "the states are merged where the rings were");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * RING];
   __shared__ float ml[NW][2][32];
@@ -553,13 +551,9 @@ __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   for (int s = 0; s < C::KS; ++s)
     qf[s] = s * 16 + g * 8 < DH ? *(const bf16x8*)(qp + s * 16 + g * 8) : bf16x8{};
   for (int e = tid; e < 3 * DH; e += NW * 64) bad[0][e] = NO_KEY;
-  if (C::FOLD) {  // the pad chunks are no lane's: K's must be zero, V's (discarded columns) are
-    ((uint32_t*)(ring + C::TILE + C::VTILE))[lane] = 0;
+  if (C::FOLD)  // the pad chunks are no lane's: K's must be zero (what V's give is discarded)
     for (int e = lane; e < C::BKV * 4; e += 64)
       ((uint32_t*)(ring + (e >> 2) * C::ROW + C::pos_k(e >> 2, C::RC) * 16))[e & 3] = 0;
-    for (int e = lane; e < C::BKV * 12; e += 64)
-      ((uint32_t*)(ring + C::TILE + e / 12 * C::VROW + C::RC * 16))[e % 12] = 0;
-  }
   __syncthreads();
 
   const lds_byte* k_at[C::KS];
