@@ -1,0 +1,55 @@
+"""The kernel instantiations of the stand-alone operators that ordinary sizes
+of test_operators_gpu.py do not reach: each case says which rule it is made for,
+and checks on the host that it meets it."""
+import pytest
+import torch
+
+from test_operators_gpu import Attn
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- fp32 attention, workgroups of 32 rows
+def many_rows(H, Hk, ql, kl, **kw):
+    """An fp32 call of at least 512 workgroups of 32 rows (query, head)."""
+    assert min(len(ql) * max(ql), sum(ql)) * (H // Hk) // 32 * Hk >= 512
+    return dict(H=H, Hk=Hk, ql=ql, kl=kl, **kw)
+
+
+F32 = [
+    many_rows(24, 24, [401, 1, 329], [401, 1, 329]),
+    many_rows(24, 8, [401, 0, 298, 5], [401, 0, 298, 5], mask="causal"),                           # odd lengths, 3 heads share keys
+    many_rows(32, 4, [333, 250], [333, 250], mask="prefix", prefix=[65, 250]),                     # 8 heads
+    many_rows(24, 8, [350, 333, 17], [33, 290, 0], room=300, mask="causal", cap=5.0, bias=True),   # rows without a key
+    many_rows(32, 2, [257, 300], [257, 300], mask="causal", cap=30.0, bias=True, std=2.0),
+    many_rows(24, 8, [690, 30], [690, 30], mask="causal", std=4.0),                                # maxima that move far
+]
+
+
+@pytest.mark.parametrize("dh", [64, 72, 128])
+@pytest.mark.parametrize("case", range(len(F32)))
+def test_attention_f32_many_rows(case, dh):
+    a = Attn("f32", dh=dh, **F32[case], seed=11 * case + dh, spare=0 if F32[case].get("room") else 3)
+    a.run()
+    a.check()
+    assert (a.o[a.q0[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dh", [64, 72, 128])
+def test_attention_f32_many_rows_what_is_not_visible_does_not_count(dh):
+    kw = many_rows(24, 24, [400, 333], [390, 333], room=400, mask="causal")
+    a, b = (Attn("f32", dh=dh, **kw, seed=3, fused=False) for _ in range(2))
+    for t in (a.k, a.v):
+        for lo, hi in ((390, 400), (733, 800)):
+            t[lo:hi:3], t[lo + 1:hi:3], t[lo + 2:hi:3] = float("nan"), float("inf"), float("-inf")
+    a.run()
+    b.run()
+    assert torch.equal(a.o, b.o)
+    b.check()
+    # a visible NaN value and infinity: exactly the rows that see their key, in their column
+    a.v[500, 5, 9], a.v[601, 6, dh - 1] = float("nan"), float("inf")
+    a.run()
+    got, want = a.o[400:].clone(), b.o[400:]
+    assert got[100:, 5, 9].isnan().all() and (got[201:, 6, dh - 1] == float("inf")).all()
+    got[100:, 5, 9], got[201:, 6, dh - 1] = want[100:, 5, 9], want[201:, 6, dh - 1]
+    assert torch.equal(got, want) and torch.equal(a.o[:400], b.o[:400])
