@@ -189,6 +189,19 @@ def test_linear_grids(dm, M, K, N, dtype, ok):
     assert ok != (dm.lib().dit_linear_fp8_workspace_bytes(s) == ctypes.c_size_t(-1).value)
 
 
+@pytest.mark.parametrize("M,K,N,dtype", [(1, 8192, 256, 2), (64, 12288, 1021, 2), (1030, 4608, 1160, 1), (1030, 4608, 1160, 0)])
+def test_linear_workspace(dm, M, K, N, dtype):
+    """Few rows of 8-bit outputs, and products divided over k, need a workspace."""
+    s = dm.LinearShape(M, K, N, 0, dtype)
+    need = dm.lib().dit_linear_fp8_workspace_bytes(s)
+    assert 0 < need < 1 << 30
+
+    def call(ws, n):
+        return dm.lib().dit_linear_fp8(ctypes.byref(s), P, P, P, P, None, P, P if dtype == 2 else None, ws, n, None)
+    assert call(P, need - 1) == WS and str(need) in dm.last_error()
+    assert call(None, need) == BAD and call(P + 16, need) == BAD and "workspace" in dm.last_error()
+
+
 def test_binding_refuses_host_tensors_wrong_types_and_sizes(dm):
     t = torch.zeros(4, 2, 64)
     with pytest.raises(ValueError):  # mixed types

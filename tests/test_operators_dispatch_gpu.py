@@ -4,7 +4,7 @@ and checks on the host that it meets it."""
 import pytest
 import torch
 
-from test_operators_gpu import Attn
+from test_operators_gpu import Attn, test_linear as check_linear
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,17 @@ def test_attention_f32_many_rows_what_is_not_visible_does_not_count(dh):
     assert got[100:, 5, 9].isnan().all() and (got[201:, 6, dh - 1] == float("inf")).all()
     got[100:, 5, 9], got[201:, 6, dh - 1] = want[100:, 5, 9], want[201:, 6, dh - 1]
     assert torch.equal(got, want) and torch.equal(a.o[:400], b.o[:400])
+
+
+# ---------------------------------------------------------------- linear layers of few rows
+# Rows up to 16, 32, 64 (1, 2 or 4 fragments of 16) and blocks of k below 16, below 32, from 32 on (4, 8, 16 waves; 8
+# where there are 4 fragments), so that every instantiation meets a partial last block, fragment or group of columns.
+FEW = [(9, 2064, 136), (16, 3968, 41), (5, 4112, 128), (31, 1936, 130), (31, 2064, 130), (29, 4112, 129), (64, 1040, 24),
+       (64, 2064, 257), (50, 8192, 40)]
+
+
+@pytest.mark.parametrize("act,dtype", [("none", "bf16"), ("gelu", "f32"), ("gelu", "e4m3")])
+@pytest.mark.parametrize("M,K,N", FEW)
+def test_linear_few_rows(M, K, N, act, dtype):
+    assert M <= 64
+    check_linear(M, K, N, act, dtype)
