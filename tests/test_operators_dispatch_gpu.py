@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import paper_2605_25550_amd as dm
-from operator_refs import U, e4m3_tol, linear as ref_linear, spread
-from test_operators_gpu import DT, Attn, close, np64, quantized, rand, test_linear as check_linear
+from operator_refs import U, e4m3_tol, linear as ref_linear, norm_residual as ref_norm, spread
+from test_operators_gpu import DT, Attn, close, i32, np64, quantized, rand, test_linear as check_linear, \
+    test_norm_residual as check_norm
 
 pytestmark = pytest.mark.gpu
 
@@ -117,3 +118,31 @@ def test_linear_outliers_that_cancel(M, K, N, dtype):
     close(np64(osc), amax / 448, atol / 448 + amax / 448 * 2.0 ** -22, "scale")
     s = spread(np64(osc), 1, M, N)
     close(got * s, want, tol + e4m3_tol(np.abs(want) + tol, s), "codes")
+
+
+# ---------------------------------------------------------------- norms
+# From 2048 rows on a wave owns a row: of up to 1536 and 2048 columns (6 and 8 chunks of 256)
+@pytest.mark.parametrize("post,pre,ydt,hdt", [("none", "rms", "f32", "f32"), ("layer", "layer", "bf16", "bf16"), ("rms", "rms", "bf16", "e4m3")])
+@pytest.mark.parametrize("R,D", [(2053, 1536), (2048, 1544), (2051, 2040), (2049, 2048)])
+def test_norm_wave_per_row(R, D, post, pre, ydt, hdt):
+    check_norm(R, D, post, pre, ydt, hdt)
+
+
+@pytest.mark.parametrize("hdt", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("R,D", [(5, 1160), (2050, 328), (3, 8192)])
+def test_norm_without_a_sub_layer(R, D, hdt):
+    """No y: the first norm of a block, modulated or not, x handed on or not."""
+    x, mod, w = rand(R, R, D), rand(1, 3, 2 * D, std=0.5), 1 + rand(2, D, std=0.2)
+    rb = [r % 3 for r in range(R)]
+    shift, scale = mod[:, :D], mod[:, D:]
+    xo, h = torch.empty_like(x), torch.empty(R, D, dtype=DT[hdt], device="cuda")
+    hs = torch.empty(R, -(-D // 128), device="cuda") if hdt == "e4m3" else None
+    s = dm.norm_shape(R, D, batch=3, pre="layer", h_dtype=hdt, res_scale=0.5, mod_stride=2 * D)
+    dm.norm_residual(s, x, xo, h, w_pre=w, shift=shift, scale=scale, row_batch=i32(rb), h_scale=hs)
+    assert torch.equal(xo, 0.5 * x)
+    _, _, want, tol = ref_norm(np64(x), None, None, None, np64(w), np64(shift)[rb], np64(scale)[rb], "none", "layer", 0.5,
+                               np.float64(np.float32(1e-6)))
+    if hdt != "e4m3":
+        return close(np64(h), want, tol + U[hdt] * (np.abs(want) + tol), "h")
+    sc = spread(np64(hs), 1, R, D)
+    close(np64(h) * sc, want, tol + e4m3_tol(np.abs(want) + tol, sc), "h")
