@@ -1,9 +1,11 @@
 """Scores and values at the ends of their types, for each kernel of the
 masked attention, against the 64-bit definitions of operator_refs.py."""
+import numpy as np
 import pytest
 import torch
 
-from test_operators_gpu import Attn
+import paper_2605_25550_amd as dm
+from test_operators_gpu import DT, Attn, i32, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +58,46 @@ def test_large_values_under_rising_scores(kernel, dh, rise):
     a.run()
     assert a.o.isfinite().all()
     a.check()
+
+
+@pytest.mark.parametrize("dtype,H,nq", [("bf16", 24, 700), ("bf16", 4, 3), ("f32", 4, 40), ("f32", 24, 700)])
+@pytest.mark.parametrize("mask", ["full", "causal"])
+def test_attention_without_any_key(dtype, H, nq, mask):
+    """Empty k and v: every query gets zeros, rows outside the documents stay."""
+    q = rand(1, nq + 2, H, 64, dtype=DT[dtype])
+    kv = torch.empty(0, H, 64, dtype=DT[dtype], device="cuda")
+    o = torch.full_like(q, 7.0)
+    s = dm.attn_shape(q, kv, kv, o, docs=2, max_q=nq, max_k=0, mask=mask)
+    dm.attention(s, q, kv, kv, o, dm.attention_workspace(s), q_start=i32([0, 1, nq]))
+    assert (o[:nq] == 0).all() and (o[nq:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 72), ("bf16", 128), ("f32", 64)])
+def test_attention_many_short_documents(dtype, dh):
+    """Thousands of documents of none to four rows, single tokens and whole ones."""
+    n = 3001
+    a = Attn(dtype, 4, 2, dh, [d % 3 for d in range(n)], [d % 5 for d in range(n)], mask="causal", fused=False, seed=dh)
+    a.run()
+    a.check()
+
+
+def test_keys_that_are_the_values():
+    """One tensor as k and v (read only)."""
+    a = Attn("bf16", 8, 2, 128, [300, 40], [300, 40], fused=False, seed=1)
+    a.v = a.k
+    a.run()
+    a.check()
+
+
+def test_norm_rows_of_no_batch():
+    """A row_batch out of range is cut to the modulation's rows."""
+    R, D, B = 9, 264, 3
+    x, mod = rand(1, R, D), rand(2, B, 3 * D, std=0.5)
+    at = [-1, 0, 1, 2, 3, 2 ** 31 - 1, -2 ** 31, 100, 1]
+    out = []
+    for rb in (at, np.clip(at, 0, B - 1).tolist()):
+        xo, h = torch.empty_like(x), torch.empty_like(x)
+        s = dm.norm_shape(R, D, batch=B, pre="rms", h_dtype="f32", mod_stride=3 * D)
+        dm.norm_residual(s, x, xo, h, y=x, gate=mod[:, :D], shift=mod[:, D:2 * D], scale=mod[:, 2 * D:], row_batch=i32(rb))
+        out.append((xo, h))
+    assert all(torch.equal(u, v) for u, v in zip(*out))
