@@ -283,7 +283,8 @@ dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, floa
  *     DIT_MASK_PREFIX  j <= i + nk - nq or j < prefix[d]
  *   o = softmax over the visible keys of s, times v
  * A query without a visible key gets zeros.  What k and v hold in rows that a
- * query cannot see (NaN and infinities included) does not reach it.  A score
+ * query cannot see (NaN and infinities included) does not reach it; a value that
+ * it sees and that is not finite leaves nothing finite in its column.  A score
  * of -inf gives its key the weight 0, and a query that has no other zeros (with
  * a cap, an infinite q.k is a score of -cap or cap).  Rows of o outside every
  * document are left as they were.  fp32 softmax and sums; in bf16 the probabilities, taken
@@ -332,7 +333,7 @@ dit_status dit_attention(const dit_attn_shape *s, const void *q, const void *k, 
 /* 8-bit floating point (OCP e4m3: 448 the largest value, no infinities) with
  * an fp32 scale for every block of 128 columns, of one row (block_rows = 1:
  * activations) or of 128 rows (block_rows = 128: weights):
- *   scale = max(amax / 448, 2^-126),  code = e4m3(x * (1 / scale))
+ *   scale = max(amax * (1 / 448), 2^-126),  code = e4m3(x * (1 / scale))
  * rounded to nearest even; the last blocks of a row or a column may be
  * partial.  NaN becomes the NaN code, in a block whose scale comes from its
  * other values; an infinity makes its block's scale infinite.

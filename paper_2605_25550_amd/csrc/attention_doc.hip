@@ -30,7 +30,7 @@
 // Bound by the matrix pipe and the vector instructions beside it (32 exponentials,
 // scalings, maxima and packs per lane and tile), which overlap in part: MFMA busy
 // 56% of the cycles at head_dim 128 (4352 queries and keys, 24 heads: 228 us, 1.02
-// PFLOP/s; clips of 12870 and 4680: 1970 us, 1.17), 28% at head_dim 72, whose
+// PFLOP/s; clips of 12870 and 4680: 1910 us, 1.21), 28% at head_dim 72, whose
 // products pad to 80 and 96 columns (4 x 1024, 16 heads: 31.6 us, 0.61 PFLOP/s; a
 // slope of 1.5 us per tile and 8 us besides).  256 rows per workgroup, because
 // each row's share of the LDS reads of K and V falls with them; four waves a
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(NW * 64, 1) void doc_attn_bf16_kernel(DocAttnArgs a
 // its own, and no barrier until the four states are merged through LDS.  4 single
 // tokens over caches of 77 to 4096 keys, 24 heads on 8 of 128: 17 us with the merge,
 // 35 MB at 2.1 TB/s, a launch, a chain of loads per tile and the second launch (6 us
-// at the rate of a large read); 256 queries and keys, 16 heads of 72: 9 us.
+// at the rate of a large read); 256 queries and keys, 16 heads of 72: 8.4 us.
 template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void doc_attn_few_kernel(DocAttnArgs a) {
   using C = DocCfg<DH>;

@@ -95,7 +95,7 @@ __device__ const u32x4 zero_chunk = {0u, 0u, 0u, 0u};
 // of a fragment read come from distinct banks.
 //
 // Bound by the LDS (fragment reads beside the DMA's writes) and, in long runs, by
-// power: 17550 x 12288 x 3072 650 us, 2.03 PFLOP/s of the 3.6 that a bare loop of
+// power: 17550 x 12288 x 3072 640 us, 2.07 PFLOP/s of the 3.6 that a bare loop of
 // these products and scalings reaches, MFMA busy 51% at 1.85 GHz; 1997 x 1152 x
 // 4608 with GELU 23.3 us, of which nine blocks of k take about 12.
 template <int BM, int BN, int WM, int WN, int OUT>  // OUT: the output's dtype
@@ -561,8 +561,8 @@ hipError_t launch_linear_fp8(const LinF8Args& a, int tile, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------ quantisation
-// Bound by memory: 12288 x 3072 bf16 weights 22 us, 5.1 TB/s (a large copy reaches
-// 4.7 to 5.0); small activations by the launch (256 x 1152: the kernel 2.3 us).
+// Bound by memory: 12288 x 3072 bf16 weights 22 us, 5.1 TB/s, the rate of a large
+// copy; small activations by the launch (256 x 1152: the kernel 2.3 us).
 // Rows: 16 lanes take the 128 columns of one block, 16 bytes of bf16 (32 of fp32)
 // each.
 template <typename T>
