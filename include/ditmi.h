@@ -406,6 +406,91 @@ dit_status dit_norm_residual(const dit_norm_shape *s, const float *x, float *x_o
                              const float *w_post, const float *gate, const float *w_pre, const float *shift,
                              const float *scale, const int32_t *row_batch, void *h, float *h_scale, void *stream);
 
+/* Queries and keys between their projection and attention, in one pass: every
+ * head normed on its own and turned by the positions of its row (a rotation of
+ * pairs of its elements: rows and columns of an image; frames, rows and columns
+ * of a video; one axis of text).  For row r, head h and x = q or k:
+ *   n = norm(x) * w                     (DIT_NORM_LAYER, DIT_NORM_RMS with eps, as
+ *                                       dit_norm_residual, over head_dim; or NONE)
+ *   t = pos[r, axis of p] * freqs[p]    (radians, in 64 bits)
+ *   (n_a, n_b) = (n_a cos t - n_b sin t, n_a sin t + n_b cos t)    for pair p
+ * Pair p are the elements (2p, 2p + 1) with DIT_PAIR_NEIGHBOURS and (p, p + P) with
+ * DIT_PAIR_HALVES, P the number of all pairs; the first pairs[0] belong to axis 0,
+ * the next pairs[1] to axis 1 and so on.  Elements from 2P on are not turned.
+ * Statistics, weights and rotation in fp32, one rounding at the end; the squares of
+ * a head must not overflow fp32.
+ * Row r of q goes to row q_dst[r] of q_out (r itself without q_dst), row r of k and
+ * of v, which is copied as it is, to row k_dst[r] of k_out and v_out: the rooms of
+ * a cache, or a joint sequence.  A row whose destination lies outside of the output
+ * is not written; of two rows with one destination either's pieces may stay.  Other
+ * rows of the outputs are left as they were.  q_out may be q itself (k_out k, v_out
+ * v), with the same strides and without q_dst (k_dst).
+ *   rows >= 0 (at most 2^24);  heads, kv_heads >= 0 (either may be 0: then its
+ *              tensors are not read and may be NULL);  head_dim a multiple of 8 in
+ *              8 .. 256
+ *   q_out_rows, k_out_rows   rows of q_out; of k_out and v_out
+ *   dtype      of q, k, v and the outputs: DIT_F32 or DIT_BF16
+ *   axes       0 .. 4;  pairs of each, together at most head_dim / 2 (a multiple of
+ *              4 with DIT_PAIR_HALVES)
+ *   *_row, *_head   strides as in dit_attn_shape */
+typedef enum { DIT_PAIR_NEIGHBOURS = 0, DIT_PAIR_HALVES = 1 } dit_pairing;
+typedef struct {
+  int32_t rows, heads, kv_heads, head_dim;
+  int32_t q_out_rows, k_out_rows;
+  int32_t dtype, norm, pairing, axes;
+  int32_t pairs[4];
+  float eps;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  int64_t q_out_row, q_out_head, k_out_row, k_out_head, v_out_row, v_out_head;
+} dit_qk_shape;
+
+/*   v, v_out   both or neither
+ *   w_q, w_k   [head_dim] fp32 or NULL (ones)
+ *   pos        [rows, axes] int32;  freqs [P] fp64 (both NULL without pairs)
+ *   q_dst, k_dst   [rows] int32 or NULL */
+dit_status dit_qk_norm_rope(const dit_qk_shape *s, const void *q, const void *k, const void *v, void *q_out, void *k_out,
+                            void *v_out, const float *w_q, const float *w_k, const int32_t *pos, const double *freqs,
+                            const int32_t *q_dst, const int32_t *k_dst, void *stream);
+
+/* Microscaled 4-bit floating point (OCP MXFP4: e2m1 codes of 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives, a power of two for every 32 columns of a row):
+ *   scale = the least 2^e, e >= -127, with amax / scale < 7
+ *   code  = e2m1(x / scale), to nearest, ties to even
+ * so that the largest value rounds to 6 at most and none is off by more than half
+ * a step.  A NaN or an infinity makes its block's scale the stored value 255, which
+ * is not a number.
+ *   x      [rows, cols] of dtype (fp32 or bf16), rows x_row elements apart
+ *   codes  [rows, cols / 2] bytes, the even column in the lower four bits, contiguous
+ *   scale  [ceil(cols / 256), rows, 8] bytes e + 127 (e8m0), contiguous: block b of
+ *          row r at [b / 8, r, b % 8], so that what a tile of a product reads at
+ *          once lies together; 0 behind the last column
+ *   cols   a multiple of 32, x_row of 8;  rows >= 0 */
+dit_status dit_quantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const void *x, int64_t x_row, void *codes, void *scale,
+                            void *stream);
+
+/* The values of such codes and scales, x = code * scale (exact in fp32, and in bf16
+ * where it has them; past the largest of x's type an infinity). */
+dit_status dit_dequantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const void *codes, const void *scale, void *x,
+                              int64_t x_row, void *stream);
+
+/* A linear layer on such operands:
+ *   y[m, n] = act(sum_k a[m, k] a_scale[m, k/32] * w[n, k] w_scale[n, k/32] + bias[n])
+ * with products and their sums in fp32 on the 4-bit matrix pipe.
+ *   rows >= 0, in a multiple of 32, out >= 1
+ *   act    as dit_linear_fp8
+ *   dtype  of out: DIT_F32, DIT_BF16, or DIT_MXFP4, which quantises every row of y
+ *          anew (as dit_quantize_fp4) into out and out_scale; out a multiple of 32 */
+#define DIT_MXFP4 3
+size_t dit_linear_fp4_workspace_bytes(const dit_linear_shape *s);
+
+/*   a [rows, in / 2], w [out, in / 2] codes; a_scale [ceil(in / 256), rows, 8],
+ *   w_scale [ceil(in / 256), out, 8]; bias [out] or NULL (fp32 for DIT_F32, else
+ *   bf16); out [rows, out] ([rows, out / 2] codes for DIT_MXFP4); out_scale
+ *   [ceil(out / 256), rows, 8] for DIT_MXFP4, else NULL.  All contiguous.  Scales
+ *   behind the last column of an operand are not used. */
+dit_status dit_linear_fp4(const dit_linear_shape *s, const void *a, const void *a_scale, const void *w, const void *w_scale,
+                          const void *bias, void *out, void *out_scale, void *workspace, size_t ws_bytes, void *stream);
+
 /* Kernel timing hook for measurement.  dit_timing_enable() (host allocation
  * of HIP events, not a compute call) makes every later launch of kernel class
  * `kclass` record a start/stop hipEvent pair on its launch stream (timing-only

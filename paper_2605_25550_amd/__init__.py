@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("DITMI_LIB") or os.path.join(_HERE, "libditmi.so")
 
 DIT_OK, DIT_ERR_INVALID_ARG, DIT_ERR_UNSUPPORTED, DIT_ERR_WORKSPACE, DIT_ERR_HIP = 0, -1, -2, -3, -4
-DIT_F32, DIT_BF16, DIT_E4M3 = 0, 1, 2
+DIT_F32, DIT_BF16, DIT_E4M3, DIT_MXFP4 = 0, 1, 2, 3
 DIT_WS_BLOCK, DIT_WS_STEP, DIT_WS_COND, DIT_WS_SAMPLE, DIT_WS_SERVE = 0, 1, 2, 3, 4
 NOALLOC_SCRATCH_BYTES = 128 << 20  # DIT_NOALLOC_SCRATCH_BYTES of include/ditmi.h
 KERNEL_CLASSES = {"gemm_qkv": 0, "attention": 1, "gemm_out": 2, "gemm_fc1": 3, "gemm_fc2": 4,
@@ -29,7 +29,8 @@ KERNEL_CLASSES = {"gemm_qkv": 0, "attention": 1, "gemm_out": 2, "gemm_fc1": 3, "
 STREAM_FIELDS = ("w_ada", "b_ada", "w_qkv", "b_qkv", "w_o", "b_o", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
 C_API = ("dit_workspace_bytes", "dit_block_forward", "dit_block_forward_noalloc", "dit_step_forward", "dit_sample_euler", "dit_serve", "dit_cond_embed", "dit_pos_embed_2d",
          "dit_attention", "dit_attention_workspace_bytes", "dit_quantize_fp8", "dit_linear_fp8",
-         "dit_linear_fp8_workspace_bytes", "dit_norm_residual",
+         "dit_linear_fp8_workspace_bytes", "dit_norm_residual", "dit_qk_norm_rope", "dit_quantize_fp4", "dit_dequantize_fp4",
+         "dit_linear_fp4", "dit_linear_fp4_workspace_bytes",
          "dit_timing_enable", "dit_timing_read", "dit_timing_disable", "dit_status_string", "dit_last_error",
          "dit_version")
 
@@ -88,6 +89,14 @@ class NormShape(ctypes.Structure):
                [("eps", ctypes.c_float), ("res_scale", ctypes.c_float), ("mod_stride", ctypes.c_int64)]
 
 
+class QkShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "heads", "kv_heads", "head_dim", "q_out_rows", "k_out_rows", "dtype",
+                                              "norm", "pairing", "axes")] + \
+               [("pairs", ctypes.c_int32 * 4), ("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "q_out_row",
+                                              "q_out_head", "k_out_row", "k_out_head", "v_out_row", "v_out_head")]
+
+
 def lib() -> ctypes.CDLL:
     """Load libditmi.so (raises if it has not been built)."""
     global _LIB
@@ -115,13 +124,19 @@ def lib() -> ctypes.CDLL:
     L.dit_linear_fp8_workspace_bytes.argtypes = [P(LinearShape)]
     L.dit_linear_fp8.argtypes = [P(LinearShape)] + [vp] * 8 + [sz, vp]
     L.dit_norm_residual.argtypes = [P(NormShape)] + [vp] * 12
+    L.dit_qk_norm_rope.argtypes = [P(QkShape)] + [vp] * 13
+    L.dit_quantize_fp4.argtypes = [i32, i32, i32, vp, ctypes.c_int64, vp, vp, vp]
+    L.dit_dequantize_fp4.argtypes = [i32, i32, i32, vp, vp, vp, ctypes.c_int64, vp]
+    L.dit_linear_fp4_workspace_bytes.argtypes = [P(LinearShape)]
+    L.dit_linear_fp4.argtypes = [P(LinearShape)] + [vp] * 8 + [sz, vp]
     L.dit_attention_workspace_bytes.restype = L.dit_linear_fp8_workspace_bytes.restype = sz
+    L.dit_linear_fp4_workspace_bytes.restype = sz
     L.dit_timing_enable.argtypes = [ctypes.c_int, ctypes.c_int]
     L.dit_timing_read.argtypes = [P(ctypes.c_double), P(ctypes.c_int), P(ctypes.c_double), P(ctypes.c_double)]
     L.dit_timing_disable.argtypes = []
     for fn in ("dit_block_forward", "dit_block_forward_noalloc", "dit_step_forward", "dit_cond_embed", "dit_pos_embed_2d", "dit_timing_enable",
                "dit_timing_read", "dit_timing_disable", "dit_attention", "dit_quantize_fp8", "dit_linear_fp8",
-               "dit_norm_residual"):
+               "dit_norm_residual", "dit_qk_norm_rope", "dit_quantize_fp4", "dit_dequantize_fp4", "dit_linear_fp4"):
         getattr(L, fn).restype = ctypes.c_int
     L.dit_status_string.argtypes = [ctypes.c_int]
     L.dit_status_string.restype = ctypes.c_char_p
@@ -334,11 +349,12 @@ def pos_embed_2d(grid_h: int, grid_w: int, hidden: int, pos: torch.Tensor, strea
 
 # ---------------------------------------------------------------- stand-alone operators
 _DTYPE_IDS = {torch.float32: DIT_F32, torch.bfloat16: DIT_BF16, torch.float8_e4m3fn: DIT_E4M3}
-_TORCH_DTYPES = (torch.float32, torch.bfloat16, torch.float8_e4m3fn)
-_DTYPE_NAMES = {"f32": DIT_F32, "bf16": DIT_BF16, "e4m3": DIT_E4M3}
+_TORCH_DTYPES = (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.uint8)  # two MXFP4 codes in a byte
+_DTYPE_NAMES = {"f32": DIT_F32, "bf16": DIT_BF16, "e4m3": DIT_E4M3, "fp4": DIT_MXFP4}
 _MASKS = {"full": 0, "causal": 1, "prefix": 2}
 _NORMS = {"none": 0, "layer": 1, "rms": 2}
 _ACTS = {"none": 0, "gelu": 1}
+_PAIRINGS = {"interleaved": 0, "halves": 1}
 
 
 def _pick(table, key, what):
@@ -477,8 +493,8 @@ def quantize_fp8(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, bloc
 
 
 def linear_shape(rows: int, in_features: int, out_features: int, act: str = "none", dtype: str = "bf16") -> LinearShape:
-    """Shape struct of linear_fp8: act "none" or "gelu", dtype of the output
-    "bf16", "f32" or "e4m3"."""
+    """Shape struct of linear_fp8 and linear_fp4: act "none" or "gelu", dtype of the
+    output "bf16", "f32", or "e4m3" (linear_fp8), "fp4" (linear_fp4)."""
     return LinearShape(rows, in_features, out_features, _pick(_ACTS, act, "act"), _pick(_DTYPE_NAMES, dtype, "dtype"))
 
 
@@ -542,6 +558,130 @@ def norm_residual(shape: NormShape, x: torch.Tensor, x_out: Optional[torch.Tenso
             _mod_ptr(shift, B, D, st, "shift", dev), _mod_ptr(scale, B, D, st, "scale", dev),
             _arg(row_batch, torch.int32, R, "row_batch", dev), _arg(h, _TORCH_DTYPES[s.h_dtype], n, "h", dev),
             _arg(h_scale, f32, R * -(-D // 128), "h_scale", dev))
+
+
+def rope_freqs(pairs: Sequence[int], theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """[sum(pairs)] fp64 angles per position, theta^(-i / n) for pair i of an axis with n."""
+    return torch.cat([theta ** (-torch.arange(n, dtype=torch.float64, device=device) / max(n, 1)) for n in pairs])
+
+
+def qk_shape(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
+             k_out: Optional[torch.Tensor], v: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+             norm: str = "rms", pairs: Sequence[int] = (), pairing: str = "interleaved", eps: float = 1e-6) -> QkShape:
+    """Shape struct of qk_norm_rope on tensors laid out as these: q [rows, heads,
+    head_dim], k, v [rows, kv_heads, head_dim] and their outputs of as many heads, the
+    last dimension contiguous; q with q_out, or k with k_out, may be None.  pairs: of
+    each axis of the positions; pairing "interleaved" (elements 2p, 2p + 1) or "halves"
+    (p, p + sum(pairs)); norm "none", "layer" or "rms"."""
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q or k must be given")
+    if not 0 <= len(pairs) <= 4:
+        raise ValueError(f"pairs has {len(pairs)} axes, at most 4 are supported")
+    dims = []
+    for t, o, name in ((q, q_out, "q"), (k, k_out, "k"), (v, v_out, "v")):
+        if (t is None) != (o is None):
+            raise ValueError(f"{name} and {name}_out come together")
+        for x, nm in ((t, name), (o, name + "_out")):
+            if x is None:
+                continue
+            if x.dim() != 3 or x.shape[2] != first.shape[2]:
+                raise ValueError(f"{nm} must be [rows, heads, {first.shape[-1]}] (got {tuple(x.shape)})")
+            if x.dtype != first.dtype or x.dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError(f"all tensors must be float32 or all bfloat16 (got {x.dtype} for {nm})")
+        if t is not None and (t.shape[0] != first.shape[0] or o.shape[1] != t.shape[1]):
+            raise ValueError(f"{name} is {tuple(t.shape)}, {name}_out {tuple(o.shape)}: {first.shape[0]} rows and the same heads expected")
+    if v is not None and (k is None or v.shape[1] != k.shape[1] or v_out.shape[0] != k_out.shape[0]):
+        raise ValueError("v and v_out need k and k_out of as many heads and rows")
+    dh = first.shape[2]
+
+    def strides(x):  # a stride over one element is never used, whatever torch states
+        if x is None:
+            return [0, 0]
+        return [x.stride(0) if x.shape[0] > 1 else x.shape[1] * dh, x.stride(1) if x.shape[1] > 1 else dh]
+    st = [n for x in (q, k, v, q_out, k_out, v_out) for n in strides(x)]
+    return QkShape(first.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], dh,
+                   0 if q is None else q_out.shape[0], 0 if k is None else k_out.shape[0], _DTYPE_IDS[first.dtype],
+                   _pick(_NORMS, norm, "norm"), _pick(_PAIRINGS, pairing, "pairing"), len(pairs),
+                   (ctypes.c_int32 * 4)(*pairs), eps, *st)
+
+
+def qk_norm_rope(shape: QkShape, q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
+                 k_out: Optional[torch.Tensor], v: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                 w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                 freqs: Optional[torch.Tensor] = None, q_dst: Optional[torch.Tensor] = None,
+                 k_dst: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Every head of q and k normed (w_q, w_k [head_dim] fp32) and turned by its row's
+    positions pos [rows, axes] int32 at freqs [pairs] fp64 into q_out and k_out, v
+    copied into v_out; q_dst, k_dst [rows] int32 name the rows that they go to."""
+    s = shape
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q or k must be given")
+    dt, f32, i32, dev = _TORCH_DTYPES[s.dtype], torch.float32, torch.int32, first.get_device()
+    R, H, Hk, dh, P = s.rows, s.heads, s.kv_heads, s.head_dim, sum(s.pairs[:s.axes])
+    if (q is None) != (H == 0) or (k is None) != (Hk == 0):
+        raise ValueError(f"the shape states {H} heads of q and {Hk} of k")
+
+    def ptr(t, rows, heads, name, row, head):
+        return None if t is None else _strided_ptr(t, dt, (rows, heads, dh), name, row, head, dev)
+    _launch(dev, stream, lib().dit_qk_norm_rope, ctypes.byref(s), ptr(q, R, H, "q", s.q_row, s.q_head),
+            ptr(k, R, Hk, "k", s.k_row, s.k_head), ptr(v, R, Hk, "v", s.v_row, s.v_head),
+            ptr(q_out, s.q_out_rows, H, "q_out", s.q_out_row, s.q_out_head),
+            ptr(k_out, s.k_out_rows, Hk, "k_out", s.k_out_row, s.k_out_head),
+            ptr(v_out, s.k_out_rows, Hk, "v_out", s.v_out_row, s.v_out_head), _arg(w_q, f32, dh, "w_q", dev),
+            _arg(w_k, f32, dh, "w_k", dev), _arg(pos, i32, R * s.axes, "pos", dev), _arg(freqs, torch.float64, P, "freqs", dev),
+            _arg(q_dst, i32, R, "q_dst", dev), _arg(k_dst, i32, R, "k_dst", dev))
+
+
+def _rows_arg(x: torch.Tensor, name: str):
+    """(rows, cols, row stride) of a [rows, cols] fp32 or bf16 device tensor with contiguous columns."""
+    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda:
+        raise ValueError(f"{name} must be a [rows, cols] float32 or bfloat16 device tensor (got {x.dtype} {tuple(x.shape)})")
+    if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+    return x.shape[0], x.shape[1], x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def quantize_fp4(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, stream=None) -> None:
+    """x [rows, cols] (rows may be strided) to MXFP4: codes [rows, cols / 2] uint8, the
+    even column in the lower four bits, and scales [ceil(cols / 256), rows, 8] uint8."""
+    R, C, row = _rows_arg(x, "x")
+    dev = x.get_device()
+    _launch(dev, stream, lib().dit_quantize_fp4, R, C, _DTYPE_IDS[x.dtype], x.data_ptr(), row,
+            _arg(codes, torch.uint8, R * C // 2, "codes", dev), _arg(scale, torch.uint8, -(-C // 256) * R * 8, "scale", dev))
+
+
+def dequantize_fp4(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor, stream=None) -> None:
+    """The values of MXFP4 codes and scales (as quantize_fp4 writes them) into x [rows, cols]."""
+    R, C, row = _rows_arg(x, "x")
+    dev = x.get_device()
+    _launch(dev, stream, lib().dit_dequantize_fp4, R, C, _DTYPE_IDS[x.dtype], _arg(codes, torch.uint8, R * C // 2, "codes", dev),
+            _arg(scale, torch.uint8, -(-C // 256) * R * 8, "scale", dev), x.data_ptr(), row)
+
+
+def linear_fp4_workspace(shape: LinearShape, device="cuda") -> Optional[torch.Tensor]:
+    """Workspace of linear_fp4 calls of this shape (None where none is needed)."""
+    return _workspace(lib().dit_linear_fp4_workspace_bytes(ctypes.byref(shape)), device)
+
+
+def linear_fp4(shape: LinearShape, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+               out: torch.Tensor, workspace: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               out_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out = act(a w^T + bias) on MXFP4 codes a [rows, in / 2], w [out, in / 2] and their
+    scales (quantize_fp4); bias fp32 for an fp32 output, else bf16; out [rows, out / 2]
+    with out_scale [ceil(out / 256), rows, 8] for an fp4 output."""
+    s = shape
+    M, K, N = s.rows, s.in_features, s.out_features
+    u8, f4, dev = torch.uint8, s.dtype == DIT_MXFP4, a.get_device()
+    kp = -(-K // 256) * 8
+    ws, n = _ws_arg(workspace, dev)
+    _launch(dev, stream, lib().dit_linear_fp4, ctypes.byref(s), _arg(a, u8, M * K // 2, "a", dev),
+            _arg(a_scale, u8, M * kp, "a_scale", dev), _arg(w, u8, N * K // 2, "w", dev),
+            _arg(w_scale, u8, N * kp, "w_scale", dev),
+            _arg(bias, torch.float32 if s.dtype == DIT_F32 else torch.bfloat16, N, "bias", dev),
+            _arg(out, _TORCH_DTYPES[s.dtype], M * N // (2 if f4 else 1), "out", dev),
+            _arg(out_scale, u8, -(-N // 256) * M * 8, "out_scale", dev), ws, n)
 
 
 def timing_enable(kclass: str, max_launches: int) -> None:

@@ -18,7 +18,8 @@ ARCH = "gfx950"
 
 SOURCES = ["gemm_bf16.hip", "gemm_bf16_kg.hip", "gemm_f32.hip", "attention_bf16.hip", "attention_f32.hip",
            "elementwise.hip",
-           "attention_doc.hip", "attention_doc_f32.hip", "linear_fp8.hip", "norm_residual.hip", "ditmi.cpp", "operators.cpp"]
+           "attention_doc.hip", "attention_doc_f32.hip", "linear_fp8.hip", "norm_residual.hip",
+           "linear_fp4.hip", "qk_norm_rope.hip", "ditmi.cpp", "operators.cpp"]
 HOST_SOURCES = ["ditmi.cpp", "operators.cpp"]
 PROBE = os.path.join(PKG, "gemm_probe")
 

@@ -181,6 +181,36 @@ struct NormResArgs {
   long mod_stride;
 };
 
+// ------------------------------------------------------------------ 4-bit products, a power of two for each 32
+struct LinF4Args {
+  const uint8_t *a, *w, *a_scale, *w_scale;
+  const void* bias;
+  void* out;
+  uint8_t* out_scale;
+  int M, N, K, act, dtype;  // dtype 3: MXFP4
+  float* part;
+};
+struct LinF4Plan {
+  int tile;  // 0: the kernel of few rows; -1: it would take a grid of 2^32 threads
+  size_t bytes;  // of part
+};
+LinF4Plan linear_fp4_plan(int M, int N, int K, int dtype);
+
+// ------------------------------------------------------------------ queries and keys, normed and turned
+struct QkArgs {
+  const void *q, *k, *v;
+  void *q_out, *k_out, *v_out;
+  const float *w_q, *w_k;
+  const int32_t *pos, *q_dst, *k_dst;
+  const double* freqs;
+  int rows, H, Hk, Hv, dh, norm, halves, axes, P;
+  int axis_end[3];  // pairs before the ends of the first three axes
+  int segments;     // waves that share a row
+  long q_out_rows, k_out_rows;
+  float eps;
+  long q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head, vo_row, vo_head;
+};
+
 // ------------------------------------------------------------------ launchers
 // Each returns hipSuccess or the launch error.  dtype: 0 = fp32, 1 = bf16.
 hipError_t launch_gemm_bf16(const GemmArgs& a, int epi, int tile_cfg, hipStream_t st);
@@ -224,6 +254,11 @@ hipError_t launch_quantize_fp8(int rows, int cols, int block_rows, int dtype, co
                                float* scale, hipStream_t st);
 hipError_t launch_linear_fp8(const LinF8Args& a, int tile, hipStream_t st);
 hipError_t launch_norm_residual(const NormResArgs& a, hipStream_t st);
+hipError_t launch_quantize_fp4(int rows, int cols, int dtype, const void* x, long x_row, void* codes, void* scale, hipStream_t st);
+hipError_t launch_dequantize_fp4(int rows, int cols, int dtype, const void* codes, const void* scale, void* x, long x_row,
+                                 hipStream_t st);
+hipError_t launch_linear_fp4(const LinF4Args& a, const LinF4Plan& p, hipStream_t st);
+hipError_t launch_qk_norm_rope(QkArgs a, int dtype, hipStream_t st);
 
 // Tile configurations of the bf16 GEMM (BM x BN, LDS ring depth).
 enum {

@@ -102,7 +102,55 @@ size_t attn_bytes(const dit_attn_shape* s, const DocAttnPlan& p) {
   return p.split > 1 ? (size_t)p.split * s->q_rows * s->heads * (s->head_dim + 4) * 4 : 0;
 }
 
+// ------------------------------------------------------------------ queries and keys
+dit_status check_qk(const dit_qk_shape* s) {
+  if (!s) return fail(DIT_ERR_INVALID_ARG, "shape is NULL");
+  if (s->rows < 0 || s->heads < 0 || s->kv_heads < 0 || s->heads + (long)s->kv_heads < 1 || s->q_out_rows < 0 || s->k_out_rows < 0)
+    return fail(DIT_ERR_INVALID_ARG, "rows (%d), heads (%d), kv_heads (%d), q_out_rows (%d), k_out_rows (%d) must be >= 0, one head at least",
+                s->rows, s->heads, s->kv_heads, s->q_out_rows, s->k_out_rows);
+  // (a grid has fewer than 2^32 threads: 64 for a row)
+  if (s->heads > 65535 || s->kv_heads > 65535 || s->rows > (1 << 24))
+    return fail(DIT_ERR_UNSUPPORTED, "more than 65535 heads or 2^24 rows (%d)", s->rows);
+  if (s->head_dim < 8 || s->head_dim % 8 != 0 || s->head_dim > 256)
+    return fail(DIT_ERR_UNSUPPORTED, "head_dim %d not supported (multiples of 8 up to 256)", s->head_dim);
+  if (s->dtype != DIT_F32 && s->dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d unknown", s->dtype);
+  if (s->norm < DIT_NORM_NONE || s->norm > DIT_NORM_RMS) return fail(DIT_ERR_INVALID_ARG, "norm %d unknown", s->norm);
+  if (s->pairing != DIT_PAIR_NEIGHBOURS && s->pairing != DIT_PAIR_HALVES)
+    return fail(DIT_ERR_INVALID_ARG, "pairing %d unknown", s->pairing);
+  if (s->norm != DIT_NORM_NONE && (!(s->eps > 0.f) || !isfinite(s->eps)))
+    return fail(DIT_ERR_INVALID_ARG, "eps (%g) must be finite and > 0", s->eps);
+  if (s->axes < 0 || s->axes > 4) return fail(DIT_ERR_INVALID_ARG, "axes (%d) must be 0 .. 4", s->axes);
+  long pairs = 0;
+  for (int i = 0; i < s->axes; ++i) {
+    if (s->pairs[i] < 0) return fail(DIT_ERR_INVALID_ARG, "pairs of axis %d (%d) must be >= 0", i, s->pairs[i]);
+    pairs += s->pairs[i];
+  }
+  if (pairs * 2 > s->head_dim) return fail(DIT_ERR_INVALID_ARG, "%ld pairs do not fit head_dim (%d)", pairs, s->head_dim);
+  if (s->pairing == DIT_PAIR_HALVES && pairs % 4 != 0)
+    return fail(DIT_ERR_UNSUPPORTED, "%ld pairs of halves: not a multiple of 4", pairs);
+  return DIT_OK;
+}
+
 // ------------------------------------------------------------------ linear
+LinF4Plan plan_linear4(const dit_linear_shape* s) {
+  return s->rows > 0 ? linear_fp4_plan(s->rows, s->out, s->in, s->dtype) : LinF4Plan{};
+}
+
+dit_status check_linear4(const dit_linear_shape* s) {
+  if (!s) return fail(DIT_ERR_INVALID_ARG, "shape is NULL");
+  if (s->rows < 0 || s->in < 32 || s->in % 32 != 0 || s->out < 1)
+    return fail(DIT_ERR_INVALID_ARG, "rows (%d) must be >= 0, in (%d) a positive multiple of 32, out (%d) >= 1", s->rows,
+                s->in, s->out);
+  if (s->act != DIT_ACT_NONE && s->act != DIT_ACT_GELU) return fail(DIT_ERR_INVALID_ARG, "act %d unknown", s->act);
+  if (s->dtype != DIT_F32 && s->dtype != DIT_BF16 && s->dtype != DIT_MXFP4)
+    return fail(DIT_ERR_INVALID_ARG, "dtype %d is not DIT_F32, DIT_BF16 or DIT_MXFP4", s->dtype);
+  if (s->dtype == DIT_MXFP4 && s->out % 32 != 0)
+    return fail(DIT_ERR_INVALID_ARG, "out (%d) must be a multiple of 32 for a 4-bit output", s->out);
+  if ((long)s->in > (1L << 22) || (long)s->out > (1L << 26) || (long)s->rows > (1L << 26) || plan_linear4(s).tile < 0)
+    return fail(DIT_ERR_UNSUPPORTED, "product of %d x %d x %d is too large", s->rows, s->out, s->in);
+  return DIT_OK;
+}
+
 LinF8Plan plan_linear(const dit_linear_shape* s) {
   return s->rows > 0 ? linear_fp8_plan(s->rows, s->out, s->in, s->dtype) : LinF8Plan{};
 }
@@ -333,5 +381,181 @@ dit_status dit_norm_residual(const dit_norm_shape* s, const float* x, float* x_o
   const double bytes = n * (4 + (x_out ? 4 : 0) + (y ? (s->y_dtype == DIT_BF16 ? 2 : 4) : 0) +
                             (h ? (s->h_dtype == DIT_F32 ? 4 : s->h_dtype == DIT_BF16 ? 2 : 1) : 0));
   HIP_TRY(timed(DIT_K_LN_MOD, 16 * n, bytes, st, [&]() { return launch_norm_residual(a, st); }));
+  return DIT_OK;
+}
+
+// rows [rows, cols] of quantised blocks of 32, and of the values x they stand for
+static dit_status check_blocks(int32_t rows, int32_t cols, int32_t dtype, int64_t x_row) {
+  if (rows < 0 || cols < 32 || cols % 32 != 0 || x_row % 8 != 0 || x_row < cols)
+    return fail(DIT_ERR_INVALID_ARG, "rows (%d) must be >= 0, cols (%d) a positive multiple of 32, x_row (%lld) one of 8 and >= cols",
+                rows, cols, (long long)x_row);
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  // (a grid has fewer than 2^32 threads: 256 for 8 rows of 256 columns)
+  if (x_row > (1L << 40) || cols > (1 << 30) || (((long)rows + 7) / 8) * (((long)cols + 255) / 256) >= (1L << 24))
+    return fail(DIT_ERR_UNSUPPORTED, "%d rows of %d columns are too many", rows, cols);
+  return DIT_OK;
+}
+
+dit_status dit_quantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const void* x, int64_t x_row, void* codes, void* scale,
+                            void* stream) {
+  TRY(check_blocks(rows, cols, dtype, x_row));
+  if (rows == 0) return DIT_OK;
+  TRY(check_ptr(x, "x", 16, false));
+  TRY(check_ptr(codes, "codes", 16, false));
+  TRY(check_ptr(scale, "scale", 16, false));
+  const hipStream_t st = (hipStream_t)stream;
+  const double n = (double)rows * cols;
+  HIP_TRY(timed(DIT_K_OTHER, 3 * n, n * ((dtype == DIT_BF16 ? 2 : 4) + 0.53125), st, [&]() {
+    return launch_quantize_fp4(rows, cols, dtype, x, x_row, codes, scale, st);
+  }));
+  return DIT_OK;
+}
+
+dit_status dit_dequantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const void* codes, const void* scale, void* x,
+                              int64_t x_row, void* stream) {
+  TRY(check_blocks(rows, cols, dtype, x_row));
+  if (rows == 0) return DIT_OK;
+  TRY(check_ptr(codes, "codes", 16, false));
+  TRY(check_ptr(scale, "scale", 16, false));
+  TRY(check_ptr(x, "x", 16, false));
+  const hipStream_t st = (hipStream_t)stream;
+  const double n = (double)rows * cols;
+  HIP_TRY(timed(DIT_K_OTHER, n, n * ((dtype == DIT_BF16 ? 2 : 4) + 0.53125), st, [&]() {
+    return launch_dequantize_fp4(rows, cols, dtype, codes, scale, x, x_row, st);
+  }));
+  return DIT_OK;
+}
+
+size_t dit_linear_fp4_workspace_bytes(const dit_linear_shape* s) {
+  if (check_linear4(s) != DIT_OK) return BAD_SIZE;
+  return plan_linear4(s).bytes;
+}
+
+dit_status dit_linear_fp4(const dit_linear_shape* s, const void* a, const void* a_scale, const void* w, const void* w_scale,
+                          const void* bias, void* out, void* out_scale, void* workspace, size_t ws_bytes, void* stream) {
+  TRY(check_linear4(s));
+  if (s->dtype != DIT_MXFP4 && out_scale) return fail(DIT_ERR_INVALID_ARG, "out_scale is for 4-bit outputs");
+  if (s->rows == 0) return DIT_OK;
+  TRY(check_ptr(a, "a", 16, false));
+  TRY(check_ptr(w, "w", 16, false));
+  TRY(check_ptr(a_scale, "a_scale", 16, false));
+  TRY(check_ptr(w_scale, "w_scale", 16, false));
+  TRY(check_ptr(bias, "bias", 16, true));
+  TRY(check_ptr(out, "out", 16, false));
+  TRY(check_ptr(out_scale, "out_scale", 16, s->dtype != DIT_MXFP4));
+  const LinF4Plan p = plan_linear4(s);
+  TRY(check_ws(workspace, ws_bytes, p.bytes));
+  LinF4Args l{};
+  l.a = (const uint8_t*)a;
+  l.w = (const uint8_t*)w;
+  l.a_scale = (const uint8_t*)a_scale;
+  l.w_scale = (const uint8_t*)w_scale;
+  l.bias = bias;
+  l.out = out;
+  l.out_scale = (uint8_t*)out_scale;
+  l.M = s->rows;
+  l.N = s->out;
+  l.K = s->in;
+  l.act = s->act;
+  l.dtype = s->dtype;
+  l.part = (float*)workspace;
+  const hipStream_t st = (hipStream_t)stream;
+  const double M = l.M, N = l.N, K = l.K, e = l.dtype == DIT_F32 ? 4 : l.dtype == DIT_BF16 ? 2 : 0.53125;
+  HIP_TRY(timed(DIT_K_OTHER, 2 * M * N * K, 0.53125 * K * (M + N) + M * N * e, st, [&]() { return launch_linear_fp4(l, p, st); }));
+  return DIT_OK;
+}
+
+dit_status dit_qk_norm_rope(const dit_qk_shape* s, const void* q, const void* k, const void* v, void* q_out, void* k_out,
+                            void* v_out, const float* w_q, const float* w_k, const int32_t* pos, const double* freqs,
+                            const int32_t* q_dst, const int32_t* k_dst, void* stream) {
+  TRY(check_qk(s));
+  const int unit = s->dtype == DIT_BF16 ? 8 : 4, dh = s->head_dim, R = s->rows, H = s->heads, Hk = s->kv_heads;
+  if ((v != nullptr) != (v_out != nullptr)) return fail(DIT_ERR_INVALID_ARG, "v and v_out come together");
+  if (v && Hk == 0) return fail(DIT_ERR_INVALID_ARG, "v has kv_heads heads, which are none");
+  if (s->norm == DIT_NORM_NONE && (w_q || w_k)) return fail(DIT_ERR_INVALID_ARG, "w_q and w_k need a norm");
+  struct {
+    const char* name;
+    int64_t row, head;
+    int heads, rows;
+    bool out;
+  } const t[6] = {{"q", s->q_row, s->q_head, H, R, false},
+                  {"k", s->k_row, s->k_head, Hk, R, false},
+                  {"v", s->v_row, s->v_head, v ? Hk : 0, R, false},
+                  {"q_out", s->q_out_row, s->q_out_head, H, s->q_out_rows, true},
+                  {"k_out", s->k_out_row, s->k_out_head, Hk, s->k_out_rows, true},
+                  {"v_out", s->v_out_row, s->v_out_head, v ? Hk : 0, s->k_out_rows, true}};
+  for (const auto& x : t) {
+    if (x.heads == 0) continue;
+    TRY(check_strides(x.name, x.row, x.head, x.heads, x.rows, dh, unit));
+    if (x.out && pieces_overlap(x.row, x.head, x.rows, x.heads, dh))
+      return fail(DIT_ERR_INVALID_ARG, "%s strides (%lld, %lld): rows and heads of %d elements overlap", x.name, (long long)x.row,
+                  (long long)x.head, dh);
+  }
+  if (H && !q_dst && s->q_out_rows < R)
+    return fail(DIT_ERR_INVALID_ARG, "q_out_rows (%d): %d rows do not fit without q_dst", s->q_out_rows, R);
+  if (Hk && !k_dst && s->k_out_rows < R)
+    return fail(DIT_ERR_INVALID_ARG, "k_out_rows (%d): %d rows do not fit without k_dst", s->k_out_rows, R);
+  // in place: every head is read and written by the same lanes, where it stays at its place
+  if ((H && q && q == q_out && (q_dst || s->q_row != s->q_out_row || s->q_head != s->q_out_head)) ||
+      (Hk && k && k == k_out && (k_dst || s->k_row != s->k_out_row || s->k_head != s->k_out_head)) ||
+      (v && v == v_out && (k_dst || s->v_row != s->v_out_row || s->v_head != s->v_out_head)))
+    return fail(DIT_ERR_INVALID_ARG, "in place only with the same strides and without q_dst or k_dst");
+  if (R == 0) return DIT_OK;
+  int pairs = 0, ends[4] = {};
+  for (int i = 0; i < 4; ++i) ends[i] = pairs += i < s->axes ? s->pairs[i] : 0;
+  TRY(check_ptr(q, "q", 16, H == 0));
+  TRY(check_ptr(k, "k", 16, Hk == 0));
+  TRY(check_ptr(v, "v", 16, true));
+  TRY(check_ptr(q_out, "q_out", 16, H == 0 || s->q_out_rows == 0));
+  TRY(check_ptr(k_out, "k_out", 16, Hk == 0 || s->k_out_rows == 0));
+  TRY(check_ptr(v_out, "v_out", 16, true));
+  TRY(check_ptr(w_q, "w_q", 16, true));
+  TRY(check_ptr(w_k, "w_k", 16, true));
+  TRY(check_ptr(pos, "pos", 4, pairs == 0));
+  TRY(check_ptr(freqs, "freqs", 8, pairs == 0));
+  TRY(check_ptr(q_dst, "q_dst", 4, true));
+  TRY(check_ptr(k_dst, "k_dst", 4, true));
+  QkArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.w_q = w_q;
+  a.w_k = w_k;
+  a.pos = pos;
+  a.freqs = freqs;
+  a.q_dst = q_dst;
+  a.k_dst = k_dst;
+  a.rows = R;
+  a.H = H;
+  a.Hk = Hk;
+  a.Hv = v ? Hk : 0;
+  a.dh = dh;
+  a.norm = s->norm;
+  a.halves = s->pairing == DIT_PAIR_HALVES;
+  a.axes = s->axes;
+  a.P = pairs;
+  for (int i = 0; i < 3; ++i) a.axis_end[i] = ends[i];
+  a.q_out_rows = s->q_out_rows;
+  a.k_out_rows = s->k_out_rows;
+  a.eps = s->eps;
+  a.q_row = s->q_row;
+  a.q_head = s->q_head;
+  a.k_row = s->k_row;
+  a.k_head = s->k_head;
+  a.v_row = s->v_row;
+  a.v_head = s->v_head;
+  a.qo_row = s->q_out_row;
+  a.qo_head = s->q_out_head;
+  a.ko_row = s->k_out_row;
+  a.ko_head = s->k_out_head;
+  a.vo_row = s->v_out_row;
+  a.vo_head = s->v_out_head;
+  const hipStream_t st = (hipStream_t)stream;
+  const double n = (double)R * dh;
+  HIP_TRY(timed(DIT_K_OTHER, 8 * n * (H + Hk), 2 * n * (H + Hk + a.Hv) * (s->dtype == DIT_BF16 ? 2 : 4), st,
+                [&]() { return launch_qk_norm_rope(a, s->dtype, st); }));
   return DIT_OK;
 }
