@@ -188,10 +188,12 @@ struct LinF4Args {
   void* out;
   uint8_t* out_scale;
   int M, N, K, act, dtype;  // dtype 3: MXFP4
-  float* part;
+  int split;    // > 1: the panels of k of every tile are divided into so many ranges, whose fp32 sums
+  float* part;  // go to part[range][M][N rounded up to 8]
 };
 struct LinF4Plan {
-  int tile;  // 0: the kernel of few rows; -1: it would take a grid of 2^32 threads
+  int tile;  // 0: the kernel of few rows; an id of linear_fp4.hip's tiles; -1: it would take a grid of 2^32 threads
+  int split;
   size_t bytes;  // of part
 };
 LinF4Plan linear_fp4_plan(int M, int N, int K, int dtype);

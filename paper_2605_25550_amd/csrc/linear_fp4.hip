@@ -16,6 +16,14 @@ __device__ __forceinline__ float bias_at(const LinF4Args& a, int n) {
   return OUT == 0 ? ((const float*)a.bias)[n] : bf2f(((const bf16_t*)a.bias)[n]);
 }
 
+// Stores the scale of the block from column n on, and those behind the last column.
+__device__ __forceinline__ void store_scale(const LinF4Args& a, int m, int n, uint32_t s) {
+  uint8_t* p = a.out_scale + f4_scale_at(a.M, m, n / 32);
+  *p = (uint8_t)s;
+  if (n + 32 == a.N)
+    for (int b = a.N / 32; b & 7; ++b) *++p = 0;
+}
+
 // Stores eight consecutive outputs of row m from column n on, as far as there are such.  MXFP4: the four
 // lanes of a quad hold a block of 32 (out is a multiple of 32: a block is whole or not there).
 template <int OUT>
@@ -28,12 +36,7 @@ __device__ __forceinline__ void store_y8(const LinF4Args& a, int m, int n, const
     const uint32_t s = f4_scale(max_quad(mx));
     if (m >= a.M || n >= a.N) return;
     *(uint32_t*)((uint8_t*)a.out + o / 2) = pack_f4x8(y, s);
-    if (n % 32 == 0) {
-      uint8_t* p = a.out_scale + f4_scale_at(a.M, m, n / 32);
-      *p = (uint8_t)s;
-      if (n + 32 == a.N)  // the scales behind the last column
-        for (int b = a.N / 32; b & 7; ++b) *++p = 0;
-    }
+    if (n % 32 == 0) store_scale(a, m, n, s);
     return;
   }
   if (m >= a.M || n >= a.N) return;
@@ -56,95 +59,116 @@ __device__ __forceinline__ void store_y8(const LinF4Args& a, int m, int n, const
 
 __device__ __forceinline__ i32x8 operand(u32x4 c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
 
-// A workgroup owns 16 outputs of up to 16 TM rows; its waves divide the blocks of 128 k, load fragments
-// from global memory and add their sums through LDS in order.
-template <int TM, int NW, int OUT>
+// Scales of the eight blocks of a panel as a lane needs them: those of its quarter of 128 k (or half of
+// 64) in the low byte of each word; behind the last of `left` blocks 0, 2^-127, beside which codes are nothing.
+__device__ __forceinline__ u32x2 panel_mask(int left) {
+  return u32x2{left >= 4 ? ~0u : (1u << (8 * left)) - 1u, left >= 8 ? ~0u : left <= 4 ? 0u : (1u << (8 * left - 32)) - 1u};
+}
+
+// At most 16 rows: bound by the weights' bytes, and when those are few by the launch and a chain of loads.
+// A workgroup owns 16 outputs of every row (32 where they are quantised: a block); its waves divide the
+// panels of 256 k, load fragments of v_mfma_scale_f32_16x16x128_f8f6f4 from global memory, U panels ahead,
+// and add their sums through LDS in order.  Past K a row's last bytes come again.
+template <int TN, int NW, int OUT>
 __global__ __launch_bounds__(NW * 64) void linear_f4_rows_kernel(LinF4Args a) {
-  constexpr int U = TM == 1 ? 4 : 2;  // blocks of k in flight per wave
-  __shared__ f32x4 sum[NW][TM][64];
+  constexpr int U = 2;
+  static_assert(OUT != 3 || TN == 2, "a block of 32");
+  __shared__ f32x4 sum[NW][TN][64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
-  const int n0 = blockIdx.x * 16;
-  const int KB = (a.K + 127) / 128;
+  const int n0 = blockIdx.x * 16 * TN, panels = (a.K + 255) / 256;
   const long half = a.K / 2;
-  const int wn = min(n0 + r16, a.N - 1);
-  const uint8_t* wrow = a.w + (long)wn * half;
-  const uint8_t* arow[TM];
-  int am[TM];
+  int row[TN + 1];  // of W, and the last of A
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    am[i] = min(i * 16 + r16, a.M - 1);
-    arow[i] = a.a + (long)am[i] * half;
-  }
-  f32x4 acc[TM];
+  for (int j = 0; j < TN; ++j) row[j] = min(n0 + j * 16 + r16, a.N - 1);
+  row[TN] = min(r16, a.M - 1);
+  f32x4 acc[TN];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 wf[U], af[U][TM];
-  int sw[U], sa[U][TM];
-  auto load = [&](int u, int kb) {
-    if (kb >= KB) return;
-    const int blk = kb * 4 + kq;
-    const bool in = blk * 32 < a.K;  // past the end: zeros, and a scale that is a number
-    const u32x4 z = {0u, 0u, 0u, 0u};
-    wf[u] = in ? *(const u32x4*)(wrow + blk * 16) : z;
-    sw[u] = in ? (int)a.w_scale[f4_scale_at(a.N, wn, blk)] : 0;
+  for (int j = 0; j < TN; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 fr[U][TN + 1][2];
+  u32x2 sc[U][TN + 1];
+  auto load = [&](int u, int p) {
+    if (p >= panels) return;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      af[u][i] = in ? *(const u32x4*)(arow[i] + blk * 16) : z;
-      sa[u][i] = in ? (int)a.a_scale[f4_scale_at(a.M, am[i], blk)] : 0;
+    for (int f = 0; f <= TN; ++f) {
+      const uint8_t* codes = (f < TN ? a.w : a.a) + row[f] * half;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fr[u][f][h] = *(const u32x4*)(codes + min(p * 128L + h * 64 + kq * 16, half - 16));
+      sc[u][f] = *(const u32x2*)((f < TN ? a.w_scale : a.a_scale) + ((long)p * (f < TN ? a.N : a.M) + row[f]) * 8);
     }
   };
 #pragma unroll
   for (int u = 0; u < U; ++u) load(u, wave + u * NW);
-  for (int kb = wave; kb < KB; kb += U * NW)
+  for (int p = wave; p < panels; p += U * NW)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (kb + u * NW >= KB) break;
+      if (p + u * NW >= panels) break;
+      const u32x2 mask = panel_mask(a.K / 32 - (p + u * NW) * 8);
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
-        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(wf[u]), operand(af[u][i]), acc[i], 4, 4, 0, sw[u],
-                                                                  0, sa[u][i]);
-      load(u, kb + (u + U) * NW);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(fr[u][j][h]), operand(fr[u][TN][h]), acc[j], 4, 4, 0,
+                                                                    (sc[u][j][h] & mask[h]) >> (8 * kq), 0,
+                                                                    (sc[u][TN][h] & mask[h]) >> (8 * kq));
+      load(u, p + (u + U) * NW);
     }
 #pragma unroll
-  for (int i = 0; i < TM; ++i) sum[wave][i][lane] = acc[i];
+  for (int j = 0; j < TN; ++j) sum[wave][j][lane] = acc[j];
   __syncthreads();
-  for (int i = wave; i < TM; i += NW) {
-    f32x4 y = sum[0][i][lane];
+  if (wave != 0) return;
+  // a lane: outputs 4 kq .. 4 kq + 3 of each 16, of row r16
+  float y[TN][4];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) y += sum[w][i][lane];
-    const int m = i * 16 + r16, n = n0 + kq * 4;
-    if (m >= a.M || n >= a.N) continue;
-    if (OUT == 3) {
-      *(f32x4*)(a.part + (long)m * a.N + n) = y;
-      continue;
+  for (int j = 0; j < TN; ++j) {
+    f32x4 t = sum[0][j][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) t += sum[w][j][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[j][e] = t[e];
+      if (a.bias) y[j][e] += bias_at<OUT>(a, min(n0 + j * 16 + kq * 4 + e, a.N - 1));
+      if (a.act) y[j][e] = gelu_tanh(y[j][e]);
     }
+  }
+  const int n = n0 + kq * 4;
+  if constexpr (OUT == 3) {
+    uint32_t mx = 0u;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < a.N) {
-        if (a.bias) y[e] += bias_at<OUT>(a, n + e);
-        if (a.act) y[e] = gelu_tanh(y[e]);
-        if (OUT == 0) ((float*)a.out)[(long)m * a.N + n + e] = y[e];
-        else ((bf16_t*)a.out)[(long)m * a.N + n + e] = f2bf(y[e]);
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = max(mx, abs_bits(y[j][e]));
+    const auto p16 = __builtin_amdgcn_permlane16_swap(mx, mx, false, false);
+    mx = max(p16[0], p16[1]);
+    const auto p32 = __builtin_amdgcn_permlane32_swap(mx, mx, false, false);
+    const uint32_t s = f4_scale(max(p32[0], p32[1]));
+    if (r16 >= a.M) return;
+    const float v[8] = {y[0][0], y[0][1], y[0][2], y[0][3], y[1][0], y[1][1], y[1][2], y[1][3]};
+    const uint32_t c = pack_f4x8(v, s);
+    uint8_t* o = (uint8_t*)a.out + ((long)r16 * a.N + n) / 2;
+    *(uint16_t*)o = (uint16_t)c;
+    *(uint16_t*)(o + 8) = (uint16_t)(c >> 16);
+    if (kq == 0) store_scale(a, r16, n0, s);
+  } else {
+    if (r16 >= a.M) return;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int nj = n + j * 16;
+      const long o = (long)r16 * a.N + nj;
+      if (nj < a.N && a.N % 4 == 0) {
+        if (OUT == 0) *(f32x4*)((float*)a.out + o) = f32x4{y[j][0], y[j][1], y[j][2], y[j][3]};
+        else *(u32x2*)((bf16_t*)a.out + o) = u32x2{pack_bf16x2(y[j][0], y[j][1]), pack_bf16x2(y[j][2], y[j][3])};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (nj + e < a.N) {
+            if (OUT == 0) ((float*)a.out)[o + e] = y[j][e];
+            else ((bf16_t*)a.out)[o + e] = f2bf(y[j][e]);
+          }
       }
+    }
   }
-}
-
-// Bias, activation and quantisation of fp32 sums [M][N]: a lane takes 8 columns.
-__global__ __launch_bounds__(256) void linear_f4_finish_kernel(LinF4Args a) {
-  const long groups = (long)a.M * (a.N / 8), i = (long)blockIdx.x * 256 + threadIdx.x;
-  const long at = min(i, groups - 1);  // (whole quads)
-  const int m = (int)(at / (a.N / 8)), n = (int)(at - (long)m * (a.N / 8)) * 8;
-  float y[8];
-  const float* p = a.part + (long)m * a.N + n;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    y[e] = p[e];
-    if (a.bias) y[e] += bias_at<3>(a, n + e);
-    if (a.act) y[e] = gelu_tanh(y[e]);
-  }
-  store_y8<3>(a, i < groups ? m : a.M, n, y);
 }
 
 // Order of the tiles: groups of eight row tiles x all column tiles, rows fastest, so that what runs at
@@ -163,58 +187,61 @@ __device__ __forceinline__ void dma_4s(const void* sbase, unsigned voff, unsigne
                : "memory", "m0");
 }
 
-// Many rows: a workgroup of WM x WN waves owns BM rows x BN outputs.  Stages of 128 k (64 bytes and four
-// scales per row of both operands) go HBM -> LDS by DMA into a ring of S slots; 16-byte chunk c of row r
-// lies at c ^ (r / 4 & 3), so that 16 rows of a fragment read come from distinct banks.  The weights are
-// the A operand of v_mfma_scale_f32_32x32x64_f8f6f4 and the activations the B operand: a lane holds 16
-// outputs of one activation row, block scales of both operands go in with the product.
+// Many rows: a workgroup of WM x WN waves owns BM rows x BN outputs.  Stages of 256 k (128 bytes, whole
+// cache lines, and eight scales per row of both operands) go HBM -> LDS by DMA into a ring of S slots;
+// 16-byte chunk c of row r lies at c ^ (r / 2 & 7), so that 16 rows of a fragment read come from distinct
+// banks.  The weights are the A operand of v_mfma_scale_f32_32x32x64_f8f6f4 and the activations the B
+// operand: a lane holds 16 outputs of one activation row, block scales of both operands go in with the
+// product.
+__host__ __device__ __forceinline__ int part_row(int N) { return (N + 7) & ~7; }  // of part: whole groups of eight
 template <int BM, int BN, int WM, int WN, int S, int OUT>
 __global__ __launch_bounds__(WM * WN * 64) void linear_f4_tile_kernel(LinF4Args a) {
-  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int IPW = (BM + BN) / (16 * NW);           // 1 KB DMA instructions per wave and stage
-  constexpr int SU = (BM + BN) / 64, SPW = (SU + NW - 1) / NW;  // 256-byte ones of scales
+  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, T = TM * TN, F = TN + TM;
+  constexpr int IPW = (BM + BN) / (8 * NW);   // 1 KB DMA instructions per wave and stage
+  constexpr int SU = (BM + BN) / 32, SPW = (SU + NW - 1) / NW;  // 256-byte ones of scales
   constexpr int PER = IPW + SPW;
-  constexpr int SCALES = (BM + BN) * 64, STAGE = (BM + BN) * 68;  // W rows, A rows; their scales
-  static_assert(BM % (16 * NW) == 0 && BN % (16 * NW) == 0 && BN % 64 == 0 && BM % 64 == 0 && S >= 3, "tile split");
+  constexpr int SCALES = (BM + BN) * 128, STAGE = (BM + BN) * 136;  // W rows, A rows; their scales
+  static_assert(NW % 2 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 32 == 0 && BN % 32 == 0 && S >= 2, "tile split");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S * STAGE];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, kq = lane >> 5;
   const int tiles_n = (a.N + BN - 1) / BN, tiles_m = (a.M + BM - 1) / BM;
+  const int unit = xcd_remap(blockIdx.x, tiles_m * tiles_n * a.split), part = unit / (tiles_m * tiles_n);
   int tm, tn;
-  tile_at(xcd_remap(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, &tm, &tn);
+  tile_at(unit - part * (tiles_m * tiles_n), tiles_m, tiles_n, &tm, &tn);
   const int wm = wave % WM, wn = wave / WM;
-  const int KB = (a.K + 127) / 128, half = a.K / 2;
+  const int panels = (a.K + 255) / 256, half = a.K / 2;
+  const int kb0 = (int)((long)panels * part / a.split), KB = (int)((long)panels * (part + 1) / a.split);
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
 
-  // DMA: instruction t of this wave covers rows 16 q .. 16 q + 15, q = wave + NW t, of the stage's W rows
-  // then A rows.  Past K a row's last chunk comes again: its scales there are made 0 (2^-127) below.
+  // DMA: instruction t of this wave covers rows 8 q .. 8 q + 7, q = wave + NW t, of the stage's W rows then
+  // A rows (of the scales: rows 32 q .. 32 q + 31).  Past K a row's last chunk comes again: its scales there
+  // are made 0 (2^-127) below.
   unsigned off[IPW], soff[SPW];
 #pragma unroll
   for (int t = 0; t < IPW; ++t) {
-    const int R = (wave + NW * t) * 16 + (lane >> 2);
-    off[t] = (unsigned)(t * NW * 16 < BN ? min(R, a.N - 1 - tn * BN) : min(R - BN, a.M - 1 - tm * BM)) * (unsigned)half;
+    const int R = (wave + NW * t) * 8 + (lane >> 3);
+    off[t] = (unsigned)(t * NW * 8 < BN ? min(R, a.N - 1 - tn * BN) : min(R - BN, a.M - 1 - tm * BM)) * (unsigned)half;
   }
-  int su[SPW];
 #pragma unroll
   for (int t = 0; t < SPW; ++t) {
-    su[t] = min(wave + NW * t, SU - 1);
-    const int R = su[t] * 64 + lane;
-    soff[t] = (unsigned)(su[t] * 64 < BN ? min(R, a.N - 1 - tn * BN) : min(R - BN, a.M - 1 - tm * BM)) * 8u;
+    const int u = min(wave + NW * t, SU - 1), R = u * 32 + (lane >> 1);  // (the last one more than once)
+    soff[t] = (unsigned)(u * 32 < BN ? min(R, a.N - 1 - tn * BN) : min(R - BN, a.M - 1 - tm * BM)) * 8u + (lane & 1) * 4u;
   }
-  const unsigned chunk = (unsigned)((lane & 3) ^ (lane >> 4)) * 16u;
+  const unsigned chunk = (unsigned)((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))) * 16u;
   const uint8_t* wb = a.w + (long)tn * BN * half;
   const uint8_t* ab = a.a + (long)tm * BM * half;
   auto issue_one = [&](int kb, int slot, int t) {
     const unsigned dst = lds0 + (unsigned)(slot * STAGE);
     if (t < IPW) {
-      const unsigned k = min((unsigned)kb * 64u + chunk, (unsigned)half - 16u);
-      dma_16s(t * NW * 16 < BN ? wb : ab, off[t] + k, dst + (unsigned)((wave + NW * t) * 1024));
+      const unsigned k = min((unsigned)kb * 128u + chunk, (unsigned)half - 16u);
+      dma_16s(t * NW * 8 < BN ? wb : ab, off[t] + k, dst + (unsigned)((wave + NW * t) * 1024));
     } else {
-      const int u = su[t - IPW];
-      const uint8_t* sb = u * 64 < BN ? a.w_scale + ((long)(kb >> 1) * a.N + tn * BN) * 8 : a.a_scale + ((long)(kb >> 1) * a.M + tm * BM) * 8;
-      dma_4s(sb, soff[t - IPW] + (unsigned)(kb & 1) * 4u, dst + (unsigned)(SCALES + u * 256));
+      const int u = min(wave + NW * (t - IPW), SU - 1);
+      const uint8_t* sb = u * 32 < BN ? a.w_scale + ((long)kb * a.N + tn * BN) * 8 : a.a_scale + ((long)kb * a.M + tm * BM) * 8;
+      dma_4s(sb, soff[t - IPW], dst + (unsigned)(SCALES + u * 256));
     }
   };
 
@@ -226,98 +253,100 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f4_tile_kernel(LinF4Args 
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.f;
 
-  // fragment f < TN: of W, else of A; k step s of the stage's two
+  // fragment f < TN: of W, else of A; k step s of the stage's four
   const int wrow = wn * (BN / WN) + r32, arow = BN + wm * (BM / WM) + r32;
-  const int ch0 = (kq ^ ((lane >> 2) & 3)) << 4;
-  auto frag = [&](int slot, int f, int s) {
-    const int row = f < TN ? wrow + f * 32 : arow + (f - TN) * 32;
-    return *(const u32x4*)(smem + slot * STAGE + row * 64 + (ch0 ^ (s << 5)));
-  };
-  auto scale = [&](int slot, int f) {
-    const int row = f < TN ? wrow + f * 32 : arow + (f - TN) * 32;
-    return *(const uint32_t*)(smem + slot * STAGE + SCALES + row * 4);
-  };
-  constexpr int F = TN + TM;
-  u32x4 f0[F], f1[F];
-  uint32_t raw[F], sc[F];
+  const int ch0 = (kq ^ ((lane >> 1) & 7)) << 4;
+  auto row_of = [&](int f) { return f < TN ? wrow + f * 32 : arow + (f - TN) * 32; };
+  auto frag = [&](int slot, int f, int s) { return *(const u32x4*)(smem + slot * STAGE + row_of(f) * 128 + (ch0 ^ (s << 5))); };
+  auto scale = [&](int slot, int f) { return *(const u32x2*)(smem + slot * STAGE + SCALES + row_of(f) * 8); };
+  // the order in which fragments are read: of W and of A in turn
+  auto nth = [](int u) { return u < 2 * (TN < TM ? TN : TM) ? u % 2 * TN + u / 2 : TN < TM ? u : u - TM; };
+  u32x4 fr[2][F];
+  u32x2 raw[F];
+  uint32_t sc[2][F];
 
+  // The DMA of a stage is spread over three of its four steps: a CU takes 16 cycles for an instruction, and a
+  // wave that issues them faster waits with its products.  Instruction t follows product issue_at(t) behind
+  // the barrier that frees the slot; the first EARLY thus the stage's last step, the others the next one's.
+  constexpr auto issue_at = [](int t) { return t * 3 * T / PER; };
+  constexpr int EARLY = (PER + 2) / 3;  // issue_at(t) < T
+  static_assert(issue_at(EARLY - 1) < T && issue_at(EARLY) >= T && issue_at(PER - 1) < 3 * T, "a third follows the last step");
 #pragma unroll
-  for (int p = 0; p < S - 1; ++p)
-    if (p < KB)
+  for (int p = 0; p < S; ++p)
+    if (kb0 + p < KB)
 #pragma unroll
-      for (int t = 0; t < PER; ++t) issue_one(p, p, t);
-  if (KB >= S - 1) wait_vmcnt<(S - 2) * PER>();
+      for (int t = 0; t < (p < S - 1 ? PER : EARLY); ++t) issue_one(kb0 + p, p, t);
+  if (kb0 + S <= KB) wait_vmcnt<(S - 2) * PER + EARLY>();
   else wait_vmcnt<0>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
-  for (int f = 0; f < F; ++f) f0[f] = frag(0, f, 0), raw[f] = scale(0, f);
+  for (int u = 0; u < F; ++u) {
+    const int f = nth(u);
+    fr[0][f] = frag(0, f, 0), raw[f] = scale(0, f);
+  }
 
-  int slot = 0, fill = S - 1;
-  // MORE: there is a stage S - 1 ahead to load
-  auto step = [&](int kb, auto MORE) {
-    constexpr bool more = decltype(MORE)::value;
+  int slot = 0;
+  // MORE: 2, there is a stage S ahead to load; 1, one S - 1 ahead; 0, none
+  auto stage = [&](int kb, auto MORE) {
+    constexpr int more = decltype(MORE)::value;
+    const int prev = slot == 0 ? S - 1 : slot - 1;
     const int next = slot + 1 == S ? 0 : slot + 1;
-    const int left = a.K / 32 - kb * 4;
-    const uint32_t mask = more || left >= 4 ? ~0u : (1u << (8 * left)) - 1u;
+    const int left = a.K / 32 - kb * 8;  // blocks of 32
+    const u32x2 mask = more == 2 ? u32x2{~0u, ~0u} : panel_mask(left);
 #pragma unroll
-    for (int f = 0; f < F; ++f) sc[f] = (raw[f] & mask) >> (8 * kq);
-    // the first k step, beside it the second one's fragments and the DMA of the stage S - 1 ahead
+    for (int f = 0; f < F; ++f) sc[0][f] = (raw[f][0] & mask[0]) >> (8 * kq), sc[1][f] = (raw[f][1] & mask[1]) >> (8 * kq);
 #pragma unroll
-    for (int x = 0; x < TN * TM; ++x) {
-      const int j = x / TM, i = x % TM;
-      constexpr int RP = (F + TN * TM - 1) / (TN * TM), DP = (PER + TN * TM - 1) / (TN * TM);
-#pragma unroll
-      for (int y = 0; y < RP; ++y)
-        if (x * RP + y < F) f1[x * RP + y] = frag(slot, x * RP + y, 1);
-      acc[j][i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(f0[j]), operand(f0[TN + i]), acc[j][i], 4, 4, 0, sc[j],
-                                                                  0, sc[TN + i]);
-      if (more)
-#pragma unroll
-        for (int y = 0; y < DP; ++y)
-          if (x * DP + y < PER) issue_one(kb + S - 1, fill, x * DP + y);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    // the second, in whose middle the waves meet: the next stage has landed, and nobody reads the last
-#pragma unroll
-    for (int x = 0; x < TN * TM; ++x) {
-      const int j = x / TM, i = x % TM;
-      constexpr int H = TN * TM / 2, RP = (F + H - 1) / H;
-      if (x == H) {
-        if (more) wait_vmcnt<(S - 2) * PER>();
+    for (int s = 0; s < 4; ++s) {
+      // before the last step, whose operands are in registers, the waves meet: the next stage has landed,
+      // and this one's slot may be filled again
+      if (s == 3) {
+        if (more == 2) wait_vmcnt<(S - 2) * PER>();
         else wait_vmcnt<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
-      if (x >= H)
 #pragma unroll
-        for (int y = 0; y < RP; ++y) {
-          const int u = (x - H) * RP + y, both = 2 * (TN < TM ? TN : TM);  // of W and of A in turn
-          const int f = u < both ? u % 2 * TN + u / 2 : TN < TM ? u : u - TM;
-          if (u < F) f0[f] = frag(next, f, 0), raw[f] = scale(next, f);
-        }
-      acc[j][i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(f1[j]), operand(f1[TN + i]), acc[j][i], 4, 4, 2, sc[j],
-                                                                  2, sc[TN + i]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int x = 0; x < T; ++x) {
+        const int j = x / TM, i = x % TM;
+        constexpr int RP = (F + T - 1) / T;
+#pragma unroll
+        for (int y = 0; y < RP; ++y)
+          if (x * RP + y < F) {
+            const int f = nth(x * RP + y);
+            fr[(s + 1) & 1][f] = s < 3 ? frag(slot, f, s + 1) : frag(next, f, 0);
+            if (s == 3) raw[f] = scale(next, f);
+          }
+        const uint32_t sw = sc[s >> 1][j], sa = sc[s >> 1][TN + i];
+        const i32x8 wf = operand(fr[s & 1][j]), af = operand(fr[s & 1][TN + i]);
+        acc[j][i] = s & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 2, sw, 2, sa)
+                          : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 0, sw, 0, sa);
+        const int at = ((s + 1) & 3) * T + x;  // products behind the barrier
+        if (s == 3 ? more == 2 : more >= 1)
+#pragma unroll
+          for (int t = 0; t < PER; ++t)
+            if (issue_at(t) == at) issue_one(s == 3 ? kb + S : kb + S - 1, s == 3 ? slot : prev, t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     slot = next;
-    fill = fill + 1 == S ? 0 : fill + 1;
   };
-  int kb = 0;
-  for (; kb + S - 1 < KB; ++kb) step(kb, std::true_type());
-  for (; kb < KB; ++kb) step(kb, std::false_type());
+  int kb = kb0;
+  for (; kb + S < KB; ++kb) stage(kb, std::integral_constant<int, 2>());
+  if (kb + S == KB) stage(kb++, std::integral_constant<int, 1>());
+  for (; kb < KB; ++kb) stage(kb, std::integral_constant<int, 0>());
 
   // Epilogue, 32 rows of the wave at a time through LDS, so that its code is short (it runs once, and
   // every line of it is fetched) and its stores are whole: element e of a lane is output 8 (e / 4) + 4 kq +
   // e % 4 of its row; read back, a lane has eight outputs in a row, the same ones of every row it takes.
-  constexpr int WC = BN / WN, PITCH = WC + 4, LPR = WC / 8, RPI = 64 / LPR;
-  static_assert(NW * 32 * PITCH * 4 <= S * STAGE, "the ring holds the rows");
+  constexpr int WC = BN / WN, PITCH = WC + 4, LPR = WC / 8, RPI = 64 / LPR, RB = RPI > 8 ? 32 / RPI : 4;
+  static_assert(NW * 32 * PITCH * 4 <= S * STAGE && 32 % (RB * RPI) == 0, "the ring holds the rows");
   float* rows = (float*)smem + wave * 32 * PITCH;
   const int c8 = (lane % LPR) * 8, n = tn * BN + wn * WC + c8;
   float bias[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bias[e] = a.bias ? bias_at<OUT>(a, min(n + e, a.N - 1)) : 0.f;
+  for (int e = 0; e < 8; ++e) bias[e] = a.bias && a.split == 1 ? bias_at<OUT>(a, min(n + e, a.N - 1)) : 0.f;
 #pragma unroll 1
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -331,69 +360,129 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f4_tile_kernel(LinF4Args 
                 f32x4{acc[j][ii][4 * g], acc[j][ii][4 * g + 1], acc[j][ii][4 * g + 2], acc[j][ii][4 * g + 3]};
     wave_lds_fence();
 #pragma unroll 1
-    for (int r0 = lane / LPR; r0 < 32; r0 += 4 * RPI) {  // four rows at once: one alone waits for its reads
-      f32x4 v[4][2];
+    for (int r0 = lane / LPR; r0 < 32; r0 += RB * RPI) {  // some rows at once: one alone waits for its reads
+      f32x4 v[RB][2];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < RB; ++q)
 #pragma unroll
         for (int h = 0; h < 2; ++h) v[q][h] = *(const f32x4*)(rows + (r0 + q * RPI) * PITCH + c8 + 4 * h);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < RB; ++q) {
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = v[q][e / 4][e % 4] + bias[e];
+        const int m = tm * BM + wm * (BM / WM) + i * 32 + r0 + q * RPI;
+        if (a.split > 1) {  // the range's own sums
+          if (m < a.M && n < a.N) {
+            float* o = a.part + ((long)part * a.M + m) * part_row(a.N) + n;
+            *(f32x4*)o = v[q][0], *(f32x4*)(o + 4) = v[q][1];
+          }
+          continue;
+        }
         if (a.act)
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = gelu_tanh(y[e]);
-        store_y8<OUT>(a, tm * BM + wm * (BM / WM) + i * 32 + r0 + q * RPI, n, y);
+        store_y8<OUT>(a, m, n, y);
       }
     }
     wave_lds_fence();
   }
 }
 
+// Adds the ranges of k in order and applies the epilogue: a lane takes eight outputs of a row.
+template <int OUT>
+__global__ __launch_bounds__(256) void linear_f4_join_kernel(LinF4Args a) {
+  const int per = part_row(a.N) / 8;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x, groups = (long)a.M * per;
+  const int m = (int)(i / per), n = (int)(i - (long)m * per) * 8;
+  const long at = min(i, groups - 1) * 8, stride = (long)a.M * part_row(a.N);
+  const f32x4 lo = sum_parts<8>(a.part + at, a.split, stride), hi = sum_parts<8>(a.part + at + 4, a.split, stride);
+  float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (a.bias) y[e] += bias_at<OUT>(a, min(n + e, a.N - 1));
+    if (a.act) y[e] = gelu_tanh(y[e]);
+  }
+  store_y8<OUT>(a, i < groups ? m : a.M, n, y);
+}
+
+// The plan of a product: at most 16 rows go to the kernel of few rows while their weights are few (16 x
+// 4608 x 1152 5.8 us against 7.5 in tiles, 16 x 8192 x 6144 10.4 in tiles against 13), else the tile with
+// the least estimate of
+//   `first` us for every round of workgroups (`tail` for a last one with few) and `stage` us for each of its
+//   panels of k (`light` where there are few workgroups),
+// fitted to 480 timings (16 .. 17550 rows, K of 384 .. 8192, N of 1152 .. 6144) within 4% in the mean; the
+// tile that it picks takes 1.6% more than the best of all in the mean, 15% at most.  Measured, us, in tiles
+// of 256 x 256, 192 x 256, 192 x 128, 128 x 128, 64 x 128, 64 x 64, 32 x 64:
+//   17550 x 4608 x 4608  184  199  234  223  278          4096 x 4608 x 1152  29  25  19  21  24  26
+//   1997 x 1152 x 4608    17  14   18   17   19  25        600 x 1152 x 4608  13  11  9.9  8.6  9.0  11
+//   200 x 4608 x 1152     25  20   15   12  9.7  8.6  7.8
+struct Tile {
+  int id, bm, bn, slots;
+  double first, stage, tail, light;
+};
+static const Tile tiles[] = {{256, 256, 256, 256, 8.7, 1.65, 5.3, 0.97}, {193, 192, 256, 256, 6.5, 1.40, 4.0, 0.77},
+                             {192, 192, 128, 256, 5.2, 0.74, 4.2, 0.46}, {128, 128, 128, 512, 5.0, 1.05, 2.5, 0.46},
+                             {65, 64, 128, 512, 3.4, 0.63, 2.4, 0.26},   {64, 64, 64, 512, 2.8, 0.41, 2.1, 0.22},
+                             {32, 32, 64, 1024, 3.1, 0.55, 1.8, 0.21}};
 static constexpr long MAX_THREADS = 1L << 32;  // a grid has fewer
 
 static long tiles_of(int M, int N, int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
 
 LinF4Plan linear_fp4_plan(int M, int N, int K, int dtype) {
   LinF4Plan p{};
-  if (M <= 64) {
-    if ((long)((N + 15) / 16) * 512 >= MAX_THREADS) p.tile = -1;
-    p.bytes = dtype == 3 ? (size_t)M * N * 4 : 0;
-    return p;
+  p.split = 1;
+  const int panels = (K + 255) / 256;
+  if (M <= 16 && panels < 24) return p;
+  p.tile = -1;
+  double best = 0;
+  for (const Tile& c : tiles) {
+    const long t = tiles_of(M, N, c.bm, c.bn);
+    for (int s = 1; s <= 8 && (s == 1 || (t * s <= c.slots && panels >= 4 * s)); ++s) {
+      const long wg = t * s, full = wg / c.slots, rem = wg % c.slots;
+      const double u = (double)rem / c.slots, n = (double)panels / s;
+      double us = full * (c.first + n * c.stage);
+      if (rem) us += c.tail + (c.first - c.tail) * u + n * (c.light + (c.stage - c.light) * u);
+      if (s > 1) us += 4.0 + 4e-6 * s * M * N;
+      if (wg * 512 >= MAX_THREADS || (p.tile > 0 && us >= best)) continue;
+      best = us;
+      p.tile = c.id;
+      p.split = s;
+      p.bytes = s > 1 ? (size_t)s * M * part_row(N) * 4 : 0;
+    }
   }
-  if (tiles_of(M, N, 128, 128) * 256 >= MAX_THREADS) {
-    p.tile = -1;
-    return p;
-  }
-  p.tile = tiles_of(M, N, 256, 256) >= 256 ? 256 : 128;
-  if (const char* f = getenv("F4_TILE")) p.tile = atoi(f);
   return p;
 }
 
 template <int OUT>
 static void launch_rows(const LinF4Args& a, hipStream_t st) {
-  const dim3 grid((a.N + 15) / 16), block(512);
-  if (a.M <= 16) hipLaunchKernelGGL((linear_f4_rows_kernel<1, 8, OUT>), grid, block, 0, st, a);
-  else if (a.M <= 32) hipLaunchKernelGGL((linear_f4_rows_kernel<2, 8, OUT>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((linear_f4_rows_kernel<4, 8, OUT>), grid, block, 0, st, a);
-  if (OUT == 3)
-    hipLaunchKernelGGL(linear_f4_finish_kernel, dim3((unsigned)(((long)a.M * (a.N / 8) + 255) / 256)), dim3(256), 0, st, a);
+  // 32 outputs a workgroup where 16 would give a CU two of them and each a long chain: 16 x 4608 x 4608 7.0 us
+  // against 7.7, 16 x 1152 x 12288 4.8 against 4.5
+  const int tn = OUT == 3 || (a.N > 4096 && a.K > 2048) ? 2 : 1;
+  const dim3 grid((a.N + 16 * tn - 1) / (16 * tn)), block(256);
+  if (tn == 2) hipLaunchKernelGGL((linear_f4_rows_kernel<2, 4, OUT>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((linear_f4_rows_kernel<OUT == 3 ? 2 : 1, 4, OUT>), grid, block, 0, st, a);
 }
 
 template <int BM, int BN, int WM, int WN, int S, int OUT>
 static void launch_tile(const LinF4Args& a, hipStream_t st) {
-  hipLaunchKernelGGL((linear_f4_tile_kernel<BM, BN, WM, WN, S, OUT>), dim3((unsigned)tiles_of(a.M, a.N, BM, BN)), dim3(WM * WN * 64),
-                     0, st, a);
+  hipLaunchKernelGGL((linear_f4_tile_kernel<BM, BN, WM, WN, S, OUT>), dim3((unsigned)tiles_of(a.M, a.N, BM, BN) * a.split),
+                     dim3(WM * WN * 64), 0, st, a);
+  if (a.split > 1)
+    hipLaunchKernelGGL((linear_f4_join_kernel<OUT>), dim3((unsigned)(((long)a.M * (part_row(a.N) / 8) + 255) / 256)), dim3(256), 0,
+                       st, a);
 }
 
 template <int OUT>
 static void launch_out(const LinF4Args& a, int tile, hipStream_t st) {
   if (tile == 0) launch_rows<OUT>(a, st);
-  else if (tile == 256) launch_tile<256, 256, 2, 2, 4, OUT>(a, st);
-  else if (tile == 255) launch_tile<256, 128, 2, 2, 4, OUT>(a, st);
-  else launch_tile<128, 128, 2, 2, 4, OUT>(a, st);
+  else if (tile == 256) launch_tile<256, 256, 4, 2, 2, OUT>(a, st);
+  else if (tile == 193) launch_tile<192, 256, 2, 4, 2, OUT>(a, st);
+  else if (tile == 192) launch_tile<192, 128, 2, 2, 3, OUT>(a, st);
+  else if (tile == 128) launch_tile<128, 128, 2, 2, 2, OUT>(a, st);
+  else if (tile == 65) launch_tile<64, 128, 2, 2, 3, OUT>(a, st);
+  else if (tile == 64) launch_tile<64, 64, 2, 2, 4, OUT>(a, st);
+  else launch_tile<32, 64, 1, 2, 4, OUT>(a, st);
 }
 
 hipError_t launch_linear_fp4(const LinF4Args& a, const LinF4Plan& p, hipStream_t st) {

@@ -458,6 +458,7 @@ dit_status dit_linear_fp4(const dit_linear_shape* s, const void* a, const void* 
   l.K = s->in;
   l.act = s->act;
   l.dtype = s->dtype;
+  l.split = p.split;
   l.part = (float*)workspace;
   const hipStream_t st = (hipStream_t)stream;
   const double M = l.M, N = l.N, K = l.K, e = l.dtype == DIT_F32 ? 4 : l.dtype == DIT_BF16 ? 2 : 0.53125;
