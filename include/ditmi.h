@@ -432,6 +432,7 @@ dit_status dit_norm_residual(const dit_norm_shape *s, const float *x, float *x_o
  *   dtype      of q, k, v and the outputs: DIT_F32 or DIT_BF16
  *   axes       0 .. 4;  pairs of each, together at most head_dim / 2 (a multiple of
  *              4 with DIT_PAIR_HALVES)
+ *   eps        at least 2^-126
  *   *_row, *_head   strides as in dit_attn_shape */
 typedef enum { DIT_PAIR_NEIGHBOURS = 0, DIT_PAIR_HALVES = 1 } dit_pairing;
 typedef struct {

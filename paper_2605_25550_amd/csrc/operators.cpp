@@ -117,8 +117,8 @@ dit_status check_qk(const dit_qk_shape* s) {
   if (s->norm < DIT_NORM_NONE || s->norm > DIT_NORM_RMS) return fail(DIT_ERR_INVALID_ARG, "norm %d unknown", s->norm);
   if (s->pairing != DIT_PAIR_NEIGHBOURS && s->pairing != DIT_PAIR_HALVES)
     return fail(DIT_ERR_INVALID_ARG, "pairing %d unknown", s->pairing);
-  if (s->norm != DIT_NORM_NONE && (!(s->eps > 0.f) || !isfinite(s->eps)))
-    return fail(DIT_ERR_INVALID_ARG, "eps (%g) must be finite and > 0", s->eps);
+  if (s->norm != DIT_NORM_NONE && (!(s->eps >= 0x1p-126f) || !isfinite(s->eps)))
+    return fail(DIT_ERR_INVALID_ARG, "eps (%g) must be finite and at least 2^-126", s->eps);
   if (s->axes < 0 || s->axes > 4) return fail(DIT_ERR_INVALID_ARG, "axes (%d) must be 0 .. 4", s->axes);
   long pairs = 0;
   for (int i = 0; i < s->axes; ++i) {

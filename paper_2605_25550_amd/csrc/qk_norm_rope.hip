@@ -19,129 +19,139 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// Eight values of a head as they lie in memory: a piece of four at p, another at p + gap.
-template <typename T>
-struct Raw;
-template <>
-struct Raw<bf16_t> {
-  u32x2 lo, hi;
-  __device__ void load(const bf16_t* p, int gap) { lo = *(const u32x2*)p, hi = *(const u32x2*)(p + gap); }
-  __device__ void store(bf16_t* p, int gap) const { *(u32x2*)p = lo, *(u32x2*)(p + gap) = hi; }
+// Eight values of a head as they lie in memory: neighbours, or (HALVES) a piece of four at p and another
+// at p + gap.
+template <typename T, bool HALVES>
+struct Raw {
+  static constexpr int N = sizeof(T) == 2 ? 2 : 4;  // dwords of a piece
+  u32x4 w[N / 2];
+
+  __device__ void load(const T* p, int gap) {
+    if constexpr (N == 4) w[0] = *(const u32x4*)p, w[1] = *(const u32x4*)(p + (HALVES ? gap : 4));
+    else if constexpr (!HALVES) w[0] = *(const u32x4*)p;
+    else {
+      const u32x2 lo = *(const u32x2*)p, hi = *(const u32x2*)(p + gap);
+      w[0] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+  }
+  __device__ void store(T* p, int gap) const {
+    if constexpr (N == 4) *(u32x4*)p = w[0], *(u32x4*)(p + (HALVES ? gap : 4)) = w[1];
+    else if constexpr (!HALVES) *(u32x4*)p = w[0];
+    else *(u32x2*)p = u32x2{w[0][0], w[0][1]}, *(u32x2*)(p + gap) = u32x2{w[0][2], w[0][3]};
+  }
   __device__ void get(float (&x)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[2 * i] = __uint_as_float(lo[i] << 16), x[2 * i + 1] = __uint_as_float(lo[i] & 0xFFFF0000u);
-      x[4 + 2 * i] = __uint_as_float(hi[i] << 16), x[5 + 2 * i] = __uint_as_float(hi[i] & 0xFFFF0000u);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (N == 4) x[i] = __uint_as_float(w[0][i]), x[4 + i] = __uint_as_float(w[1][i]);
+      else x[2 * i] = __uint_as_float(w[0][i] << 16), x[2 * i + 1] = __uint_as_float(w[0][i] & 0xFFFF0000u);
     }
   }
   __device__ void set(const float (&x)[8]) {
-    lo = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-    hi = u32x2{pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-  }
-};
-template <>
-struct Raw<float> {
-  f32x4 lo, hi;
-  __device__ void load(const float* p, int gap) { lo = *(const f32x4*)p, hi = *(const f32x4*)(p + gap); }
-  __device__ void store(float* p, int gap) const { *(f32x4*)p = lo, *(f32x4*)(p + gap) = hi; }
-  __device__ void get(float (&x)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = lo[i], x[4 + i] = hi[i];
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (N == 4) w[0][i] = __float_as_uint(x[i]), w[1][i] = __float_as_uint(x[4 + i]);
+      else w[0][i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+    }
   }
-  __device__ void set(const float (&x)[8]) { lo = f32x4{x[0], x[1], x[2], x[3]}, hi = f32x4{x[4], x[5], x[6], x[7]}; }
 };
 
-// A wave takes `seg` of a row's segments: heads chunk * (64 / LP) + lane / LP for chunk = segment,
-// segment + segments, ...; the heads of q, k and v count through.  LP lanes (a power of two, dh / 8 of
-// them at work) hold a head, lane l its pairs 4 l .. 4 l + 3: eight neighbours, or, where a head's
-// halves are paired, four of each.
+// A wave takes one of a row's segments: chunks seg, seg + segments, ... of 64 / LP heads of one tensor,
+// those of q before those of k and of v.  LP lanes (a power of two, dh / 8 of them at work) hold a head,
+// lane l its pairs 4 l .. 4 l + 3: eight neighbours, or, where a head's halves are paired, four of each.
+// The first chunk's values are on their way while the angles are made, the next chunk's while one is
+// computed.
 template <typename T, int LP, bool HALVES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   constexpr int HPW = 64 / LP;
-  const int lane = threadIdx.x & 63, l = lane & (LP - 1);
+  const int lane = threadIdx.x & 63, l = lane & (LP - 1), g = lane / LP;
   const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= (long)a.rows * a.segments) return;
-  const int row = (int)(unit / a.segments), seg = (int)(unit - (long)row * a.segments);
+  const int row = (int)((unsigned)unit / (unsigned)a.segments), seg = (int)unit - row * a.segments;
   const bool work = l < a.dh / 8;
   const int lc = work ? l : 0;
   const bool turned = lc * 4 < a.P;  // (where halves are paired P is a multiple of four)
-  const int at = HALVES ? (turned ? lc * 4 : 8 * lc) : 8 * lc;
-  const int gap = HALVES ? (turned ? a.P : 4) : 4;
+  const int at = HALVES && turned ? lc * 4 : 8 * lc;
+  const int gap = HALVES && turned ? a.P : 4;
 
-  // cos and sin of the lane's four pairs: the angle in turns, in 64 bits, less its whole turns
-  float c[4], s[4];
-  bool rot[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int p = lc * 4 + j;
-    rot[j] = p < a.P;
-    if (rot[j]) {
-      int axis = 0;
-#pragma unroll
-      for (int i = 0; i < 3; ++i) axis += p >= a.axis_end[i] ? 1 : 0;
-      double t = (double)a.pos[(long)row * a.axes + axis] * (a.freqs[p] * 0.15915494309189533577);
-      t -= rint(t);
-      if (sizeof(T) == 2) {
-        c[j] = __builtin_amdgcn_cosf((float)t), s[j] = __builtin_amdgcn_sinf((float)t);
-      } else {
-        sincospif((float)(2 * t), &s[j], &c[j]);
-      }
-    } else {
-      c[j] = 1.f, s[j] = 0.f;
-    }
-  }
-  const int heads = a.H + a.Hk + a.Hv, chunks = (heads + HPW - 1) / HPW;
+  const int cq = (a.H + HPW - 1) / HPW, ck = (a.Hk + HPW - 1) / HPW, chunks = cq + ck + (a.Hv + HPW - 1) / HPW;
   const long qd = a.q_dst ? a.q_dst[row] : row, kd = a.k_dst ? a.k_dst[row] : row;
   const bool q_in = qd >= 0 && qd < a.q_out_rows, k_in = kd >= 0 && kd < a.k_out_rows;
-  const float rdh = 1.f / (float)a.dh;
-  float wq[8], wk[8];
+  Raw<T, HALVES> raw;
+  auto load = [&](int chunk) {
+    const bool is_q = chunk < cq, is_k = chunk < cq + ck;  // (the same for the whole wave, as all of this but g and at)
+    const int h0 = (is_q ? chunk : is_k ? chunk - cq : chunk - cq - ck) * HPW, last = (is_q ? a.H : a.Hk) - 1;
+    const T* p = (const T*)(is_q ? a.q : is_k ? a.k : a.v) + row * (is_q ? a.q_row : is_k ? a.k_row : a.v_row);
+    raw.load(p + min(h0 + g, last) * (is_q ? a.q_head : is_k ? a.k_head : a.v_head) + at, gap);
+  };
+  load(seg);
+
+  const f32x4 one = {1.f, 1.f, 1.f, 1.f};
+  f32x4 wq[2] = {one, one}, wk[2] = {one, one};
+  if (a.w_q) wq[0] = *(const f32x4*)(a.w_q + at), wq[1] = *(const f32x4*)(a.w_q + at + gap);
+  if (a.w_k) wk[0] = *(const f32x4*)(a.w_k + at), wk[1] = *(const f32x4*)(a.w_k + at + gap);
+
+  // cos and sin of the lane's four pairs: the angle in turns, in 64 bits, less its whole turns
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (a.P) {
+    int pos[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int e = at + (i < 4 ? i : gap + i - 4);
-    wq[i] = a.w_q ? a.w_q[e] : 1.f;
-    wk[i] = a.w_k ? a.w_k[e] : 1.f;
-  }
-  for (int chunk = seg; chunk < chunks; chunk += a.segments) {
-    const int h = chunk * HPW + lane / LP, hc = min(h, heads - 1);
-    const int kind = hc < a.H ? 0 : hc < a.H + a.Hk ? 1 : 2;
-    const int hh = kind == 0 ? hc : kind == 1 ? hc - a.H : hc - a.H - a.Hk;
-    const T* src = (const T*)(kind == 0 ? a.q : kind == 1 ? a.k : a.v);
-    T* dst = (T*)(kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out);
-    src += row * (kind == 0 ? a.q_row : kind == 1 ? a.k_row : a.v_row) + hh * (kind == 0 ? a.q_head : kind == 1 ? a.k_head : a.v_head) + at;
-    dst += (kind == 0 ? qd : kd) * (kind == 0 ? a.qo_row : kind == 1 ? a.ko_row : a.vo_row) +
-           hh * (kind == 0 ? a.qo_head : kind == 1 ? a.ko_head : a.vo_head) + at;
-    Raw<T> raw;
-    raw.load(src, gap);
-    float x[8];
-    raw.get(x);
-    if (a.norm) {
-      float mu = 0.f;
-      if (a.norm == 1) {
-        float t = 0.f;
+    for (int i = 0; i < 4; ++i) pos[i] = a.pos[(long)row * a.axes + min(i, a.axes - 1)];
+    double f[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t += x[i];
-        mu = group_sum<LP>(work ? t : 0.f) * rdh;
-      }
-      float t = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] -= mu;
-        t = fmaf(x[i], x[i], t);
-      }
-      const float r = 1.f / sqrtf(group_sum<LP>(work ? t : 0.f) * rdh + a.eps);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= r * (kind == 0 ? wq[i] : wk[i]);
-    }
+    for (int j = 0; j < 4; ++j) f[j] = a.freqs[min(lc * 4 + j, a.P - 1)];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int i0 = HALVES ? j : 2 * j, i1 = HALVES ? 4 + j : 2 * j + 1;
-      const float u = x[i0], v = x[i1];
-      x[i0] = rot[j] ? u * c[j] - v * s[j] : u;
-      x[i1] = rot[j] ? u * s[j] + v * c[j] : v;
+      const int p = lc * 4 + j;
+      const int at_axis = p < a.axis_end[0] ? pos[0] : p < a.axis_end[1] ? pos[1] : p < a.axis_end[2] ? pos[2] : pos[3];
+      double t = (double)at_axis * (f[j] * 0.15915494309189533577);
+      t -= rint(t);
+      if (sizeof(T) == 2) c[j] = __builtin_amdgcn_cosf((float)t), s[j] = __builtin_amdgcn_sinf((float)t);
+      else sincospif((float)(2 * t), &s[j], &c[j]);
     }
-    Raw<T> out = raw;
-    if (kind != 2) out.set(x);
-    if (work && h < heads && (kind == 0 ? q_in : k_in)) out.store(dst, gap);
+  }
+  const bool whole = 2 * a.P == a.dh;
+  const float rdh = 1.f / (float)a.dh;
+  for (int chunk = seg; chunk < chunks; chunk += a.segments) {
+    const bool is_q = chunk < cq, is_k = chunk < cq + ck;
+    const int h = (is_q ? chunk : is_k ? chunk - cq : chunk - cq - ck) * HPW + g;
+    Raw<T, HALVES> out = raw;
+    if (chunk + a.segments < chunks) load(chunk + a.segments);
+    if (is_k) {  // (not v)
+      float x[8];
+      out.get(x);
+      if (a.norm) {
+        float mu = 0.f;
+        if (a.norm == 1) {
+          const float t = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+          mu = group_sum<LP>(work ? t : 0.f) * rdh;
+        }
+        // (not inside the branch: the compiler lost the values of the other path there)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] -= mu;
+        float t = x[0] * x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) t = fmaf(x[i], x[i], t);
+        // (eps is a normal number: so is what the root is taken of)
+        const float r = __builtin_amdgcn_rsqf(group_sum<LP>(work ? t : 0.f) * rdh + a.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= r * (is_q ? wq[i / 4][i % 4] : wk[i / 4][i % 4]);
+      }
+      if (a.P)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i0 = HALVES ? j : 2 * j, i1 = HALVES ? 4 + j : 2 * j + 1;
+          const float u = x[i0], v = x[i1];
+          x[i0] = u * c[j] - v * s[j];
+          x[i1] = u * s[j] + v * c[j];
+          if (!whole && lc * 4 + j >= a.P) x[i0] = u, x[i1] = v;  // (what is not turned may be infinite)
+        }
+      out.set(x);
+    }
+    const bool in = is_q ? q_in : k_in;
+    if (in && work && h < (is_q ? a.H : a.Hk)) {
+      T* p = (T*)(is_q ? a.q_out : is_k ? a.k_out : a.v_out) + (is_q ? qd * a.qo_row : kd * (is_k ? a.ko_row : a.vo_row));
+      out.store(p + h * (is_q ? a.qo_head : is_k ? a.ko_head : a.vo_head) + at, gap);
+    }
   }
 }
 
@@ -163,10 +173,11 @@ hipError_t launch_qk_norm_rope(QkArgs a, int dtype, hipStream_t st) {
   const int lanes = a.dh / 8;
   int lp = 1;
   while (lp < lanes) lp *= 2;
-  const int hpw = 64 / lp, chunks = (a.H + a.Hk + a.Hv + hpw - 1) / hpw;
-  // enough waves to fill the card
-  const long want = (16384 + a.rows - 1) / a.rows;
-  a.segments = (int)(want < chunks ? want : chunks);
+  const int hpw = 64 / lp, chunks = (a.H + hpw - 1) / hpw + (a.Hk + hpw - 1) / hpw + (a.Hv + hpw - 1) / hpw;
+  // four waves per SIMD, and no wave with more than six chunks: 17550 rows of 24 + 24 heads of 128 85 us in
+  // two segments against 91 in one; 3431 rows of 16 + 16 of 72 14.0 in two, 18.0 in eight
+  const int fill = (4096 + a.rows - 1) / a.rows, most = (chunks + 5) / 6;
+  a.segments = fill > chunks ? chunks : fill > most ? fill : most;
   if (dtype == 0) a.halves ? launch_qk<float, true>(a, st) : launch_qk<float, false>(a, st);
   else a.halves ? launch_qk<bf16_t, true>(a, st) : launch_qk<bf16_t, false>(a, st);
   return hipGetLastError();

@@ -31,7 +31,7 @@ def call_qk(dm, s, q=Q, k=K, v=V, q_out=QO, k_out=KO, v_out=VO, w_q=P, w_k=P, po
     (dict(rows=-1), BAD), (dict(heads=-1), BAD), (dict(kv_heads=-1), BAD), (dict(q_out_rows=-1), BAD), (dict(k_out_rows=-1), BAD),
     (dict(heads=0, kv_heads=0), BAD), (dict(heads=65536), UNSUP), (dict(rows=(1 << 24) + 1, q_out_rows=1 << 25), UNSUP),
     (dict(head_dim=60), UNSUP), (dict(head_dim=0), UNSUP), (dict(head_dim=264), UNSUP), (dict(dtype=2), BAD), (dict(dtype=-1), BAD),
-    (dict(norm=3), BAD), (dict(norm=-1), BAD), (dict(pairing=2), BAD), (dict(pairing=-1), BAD), (dict(eps=0.0), BAD),
+    (dict(norm=3), BAD), (dict(norm=-1), BAD), (dict(pairing=2), BAD), (dict(pairing=-1), BAD), (dict(eps=0.0), BAD), (dict(eps=1e-39), BAD),
     (dict(eps=float("nan")), BAD), (dict(eps=float("inf")), BAD), (dict(axes=-1), BAD), (dict(axes=5), BAD),
     (dict(pairs=(16, -1)), BAD), (dict(pairs=(16, 17)), BAD), (dict(pairs=(2 ** 31 - 1, 2 ** 31 - 1)), BAD),
     (dict(pairing=1, pairs=(16, 14)), UNSUP), (dict(q_row=500), BAD), (dict(q_row=256), True), (dict(k_head=60), BAD), (dict(v_row=32), BAD),
