@@ -424,6 +424,8 @@ def _workspace(n: int, device) -> Optional[torch.Tensor]:
 
 def _strided_ptr(t: torch.Tensor, dtype, shape, name: str, row: int, head: int, device: int):
     """Pointer of a [rows, heads, head_dim] tensor with the strides its shape struct states."""
+    if t.dtype is dtype and t.shape == shape and t.stride() == (row, head, 1) and device >= 0 and t.get_device() == device:
+        return t.data_ptr()  # (what nearly every call gives; below, strides that no element uses, and the errors)
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
     r, h, d = t.stride() if t.dim() == 3 else (0, 0, 0)
@@ -619,18 +621,22 @@ def qk_norm_rope(shape: QkShape, q: Optional[torch.Tensor], k: Optional[torch.Te
     if first is None:
         raise ValueError("q or k must be given")
     dt, f32, i32, dev = _TORCH_DTYPES[s.dtype], torch.float32, torch.int32, first.get_device()
-    R, H, Hk, dh, P = s.rows, s.heads, s.kv_heads, s.head_dim, sum(s.pairs[:s.axes])
+    R, H, Hk, dh, kr = s.rows, s.heads, s.kv_heads, s.head_dim, s.k_out_rows
     if (q is None) != (H == 0) or (k is None) != (Hk == 0):
         raise ValueError(f"the shape states {H} heads of q and {Hk} of k")
-
-    def ptr(t, rows, heads, name, row, head):
-        return None if t is None else _strided_ptr(t, dt, (rows, heads, dh), name, row, head, dev)
-    _launch(dev, stream, lib().dit_qk_norm_rope, ctypes.byref(s), ptr(q, R, H, "q", s.q_row, s.q_head),
-            ptr(k, R, Hk, "k", s.k_row, s.k_head), ptr(v, R, Hk, "v", s.v_row, s.v_head),
-            ptr(q_out, s.q_out_rows, H, "q_out", s.q_out_row, s.q_out_head),
-            ptr(k_out, s.k_out_rows, Hk, "k_out", s.k_out_row, s.k_out_head),
-            ptr(v_out, s.k_out_rows, Hk, "v_out", s.v_out_row, s.v_out_head), _arg(w_q, f32, dh, "w_q", dev),
-            _arg(w_k, f32, dh, "w_k", dev), _arg(pos, i32, R * s.axes, "pos", dev), _arg(freqs, torch.float64, P, "freqs", dev),
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q and q_out, k and k_out come together")
+    kv, kv_out = (R, Hk, dh), (kr, Hk, dh)
+    _launch(dev, stream, lib().dit_qk_norm_rope, ctypes.byref(s),
+            None if q is None else _strided_ptr(q, dt, (R, H, dh), "q", s.q_row, s.q_head, dev),
+            None if k is None else _strided_ptr(k, dt, kv, "k", s.k_row, s.k_head, dev),
+            None if v is None else _strided_ptr(v, dt, kv, "v", s.v_row, s.v_head, dev),
+            None if q is None else _strided_ptr(q_out, dt, (s.q_out_rows, H, dh), "q_out", s.q_out_row, s.q_out_head, dev),
+            None if k is None else _strided_ptr(k_out, dt, kv_out, "k_out", s.k_out_row, s.k_out_head, dev),
+            None if v_out is None else _strided_ptr(v_out, dt, kv_out, "v_out", s.v_out_row, s.v_out_head, dev),
+            _arg(w_q, f32, dh, "w_q", dev), _arg(w_k, f32, dh, "w_k", dev),
+            None if pos is None else _arg(pos, i32, R * s.axes, "pos", dev),
+            None if freqs is None else _arg(freqs, torch.float64, sum(s.pairs[:s.axes]), "freqs", dev),
             _arg(q_dst, i32, R, "q_dst", dev), _arg(k_dst, i32, R, "k_dst", dev))
 
 

@@ -261,81 +261,156 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_f4_tile_kernel(LinF4Args 
   auto scale = [&](int slot, int f) { return *(const u32x2*)(smem + slot * STAGE + SCALES + row_of(f) * 8); };
   // the order in which fragments are read: of W and of A in turn
   auto nth = [](int u) { return u < 2 * (TN < TM ? TN : TM) ? u % 2 * TN + u / 2 : TN < TM ? u : u - TM; };
-  u32x4 fr[2][F];
-  u32x2 raw[F];
-  uint32_t sc[2][F];
-
-  // The DMA of a stage is spread over three of its four steps: a CU takes 16 cycles for an instruction, and a
-  // wave that issues them faster waits with its products.  Instruction t follows product issue_at(t) behind
-  // the barrier that frees the slot; the first EARLY thus the stage's last step, the others the next one's.
-  constexpr auto issue_at = [](int t) { return t * 3 * T / PER; };
-  constexpr int EARLY = (PER + 2) / 3;  // issue_at(t) < T
-  static_assert(issue_at(EARLY - 1) < T && issue_at(EARLY) >= T && issue_at(PER - 1) < 3 * T, "a third follows the last step");
+  if constexpr (T == 1) {
+    // One product a step: too few to read the next step's operands beside them, so all of the next panel's
+    // are read beside those of one (77 x 18432 x 4608 in tiles of 32 x 64 19.8 us against 22.5; with two
+    // products a step the other order is the faster one, 9.7 us against 10.3 at 77 x 4608 x 1152).
+    u32x4 fr[2][4][F];
+    u32x2 raw[2][F];
+    auto read = [&](int slot, int b) {
 #pragma unroll
-  for (int p = 0; p < S; ++p)
-    if (kb0 + p < KB)
+      for (int f = 0; f < F; ++f) {
+        raw[b][f] = scale(slot, f);
 #pragma unroll
-      for (int t = 0; t < (p < S - 1 ? PER : EARLY); ++t) issue_one(kb0 + p, p, t);
-  if (kb0 + S <= KB) wait_vmcnt<(S - 2) * PER + EARLY>();
-  else wait_vmcnt<0>();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-#pragma unroll
-  for (int u = 0; u < F; ++u) {
-    const int f = nth(u);
-    fr[0][f] = frag(0, f, 0), raw[f] = scale(0, f);
-  }
-
-  int slot = 0;
-  // MORE: 2, there is a stage S ahead to load; 1, one S - 1 ahead; 0, none
-  auto stage = [&](int kb, auto MORE) {
-    constexpr int more = decltype(MORE)::value;
-    const int prev = slot == 0 ? S - 1 : slot - 1;
-    const int next = slot + 1 == S ? 0 : slot + 1;
-    const int left = a.K / 32 - kb * 8;  // blocks of 32
-    const u32x2 mask = more == 2 ? u32x2{~0u, ~0u} : panel_mask(left);
-#pragma unroll
-    for (int f = 0; f < F; ++f) sc[0][f] = (raw[f][0] & mask[0]) >> (8 * kq), sc[1][f] = (raw[f][1] & mask[1]) >> (8 * kq);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      // before the last step, whose operands are in registers, the waves meet: the next stage has landed,
-      // and this one's slot may be filled again
-      if (s == 3) {
-        if (more == 2) wait_vmcnt<(S - 2) * PER>();
-        else wait_vmcnt<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        for (int s = 0; s < 4; ++s) fr[b][s][f] = frag(slot, f, s);
       }
+    };
 #pragma unroll
-      for (int x = 0; x < T; ++x) {
-        const int j = x / TM, i = x % TM;
-        constexpr int RP = (F + T - 1) / T;
+    for (int p = 0; p < S; ++p)
+      if (kb0 + p < KB)
 #pragma unroll
-        for (int y = 0; y < RP; ++y)
-          if (x * RP + y < F) {
-            const int f = nth(x * RP + y);
-            fr[(s + 1) & 1][f] = s < 3 ? frag(slot, f, s + 1) : frag(next, f, 0);
-            if (s == 3) raw[f] = scale(next, f);
-          }
-        const uint32_t sw = sc[s >> 1][j], sa = sc[s >> 1][TN + i];
-        const i32x8 wf = operand(fr[s & 1][j]), af = operand(fr[s & 1][TN + i]);
-        acc[j][i] = s & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 2, sw, 2, sa)
-                          : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 0, sw, 0, sa);
-        const int at = ((s + 1) & 3) * T + x;  // products behind the barrier
-        if (s == 3 ? more == 2 : more >= 1)
+        for (int t = 0; t < PER; ++t) issue_one(kb0 + p, p, t);
+    if (kb0 + S <= KB) wait_vmcnt<(S - 1) * PER>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read(0, 0);
+    int slot = 0;
+    auto panel = [&](int kb, auto CUR, auto MORE) {  // MORE: there is a panel S ahead to load
+      constexpr int b = decltype(CUR)::value;
+      constexpr bool more = decltype(MORE)::value;
+      const int next = slot + 1 == S ? 0 : slot + 1;
+      // the waves meet: the next panel has landed, and this one, in registers, leaves its slot
+      if (more) wait_vmcnt<(S - 2) * PER>();
+      else wait_vmcnt<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      read(next, 1 - b);
+      if (more)
 #pragma unroll
-          for (int t = 0; t < PER; ++t)
-            if (issue_at(t) == at) issue_one(s == 3 ? kb + S : kb + S - 1, s == 3 ? slot : prev, t);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int t = 0; t < PER; ++t) issue_one(kb + S, slot, t);
+      const u32x2 mask = more ? u32x2{~0u, ~0u} : panel_mask(a.K / 32 - kb * 8);
+      uint32_t sc[2][F];
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sc[h][f] = (raw[b][f][h] & mask[h]) >> (8 * kq);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int x = 0; x < T; ++x) {
+          const int j = x / TM, i = x % TM;
+          const uint32_t sw = sc[s >> 1][j], sa = sc[s >> 1][TN + i];
+          const i32x8 wf = operand(fr[b][s][j]), af = operand(fr[b][s][TN + i]);
+          acc[j][i] = s & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 2, sw, 2, sa)
+                            : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 0, sw, 0, sa);
+        }
+      slot = next;
+    };
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    int kb = kb0;
+    for (; kb + 1 + S < KB; kb += 2) panel(kb, even, std::true_type()), panel(kb + 1, odd, std::true_type());
+    if (kb + S < KB) {
+      panel(kb++, even, std::true_type());
+      for (; kb < KB; kb += 2) {
+        panel(kb, odd, std::false_type());
+        if (kb + 1 < KB) panel(kb + 1, even, std::false_type());
+      }
+    } else {
+      for (; kb < KB; kb += 2) {
+        panel(kb, even, std::false_type());
+        if (kb + 1 < KB) panel(kb + 1, odd, std::false_type());
       }
     }
-    slot = next;
-  };
-  int kb = kb0;
-  for (; kb + S < KB; ++kb) stage(kb, std::integral_constant<int, 2>());
-  if (kb + S == KB) stage(kb++, std::integral_constant<int, 1>());
-  for (; kb < KB; ++kb) stage(kb, std::integral_constant<int, 0>());
+  } else {
+    u32x4 fr[2][F];
+    u32x2 raw[F];
+    uint32_t sc[2][F];
+
+    // The DMA of a stage is spread over three of its four steps: a CU takes 16 cycles for an instruction, and a
+    // wave that issues them faster waits with its products.  Instruction t follows product issue_at(t) behind
+    // the barrier that frees the slot; the first EARLY thus the stage's last step, the others the next one's.
+    constexpr auto issue_at = [](int t) { return t * 3 * T / PER; };
+    constexpr int EARLY = (PER + 2) / 3;  // issue_at(t) < T
+    static_assert(issue_at(EARLY - 1) < T && issue_at(EARLY) >= T && issue_at(PER - 1) < 3 * T, "a third follows the last step");
+#pragma unroll
+    for (int p = 0; p < S; ++p)
+      if (kb0 + p < KB)
+#pragma unroll
+        for (int t = 0; t < (p < S - 1 ? PER : EARLY); ++t) issue_one(kb0 + p, p, t);
+    if (kb0 + S <= KB) wait_vmcnt<(S - 2) * PER + EARLY>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < F; ++u) {
+      const int f = nth(u);
+      fr[0][f] = frag(0, f, 0), raw[f] = scale(0, f);
+    }
+
+    int slot = 0;
+    // MORE: 2, there is a stage S ahead to load; 1, one S - 1 ahead; 0, none
+    auto stage = [&](int kb, auto MORE) {
+      constexpr int more = decltype(MORE)::value;
+      const int prev = slot == 0 ? S - 1 : slot - 1;
+      const int next = slot + 1 == S ? 0 : slot + 1;
+      const int left = a.K / 32 - kb * 8;  // blocks of 32
+      const u32x2 mask = more == 2 ? u32x2{~0u, ~0u} : panel_mask(left);
+#pragma unroll
+      for (int f = 0; f < F; ++f) sc[0][f] = (raw[f][0] & mask[0]) >> (8 * kq), sc[1][f] = (raw[f][1] & mask[1]) >> (8 * kq);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        // before the last step, whose operands are in registers, the waves meet: the next stage has landed,
+        // and this one's slot may be filled again
+        if (s == 3) {
+          if (more == 2) wait_vmcnt<(S - 2) * PER>();
+          else wait_vmcnt<0>();
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        }
+#pragma unroll
+        for (int x = 0; x < T; ++x) {
+          const int j = x / TM, i = x % TM;
+          constexpr int RP = (F + T - 1) / T;
+#pragma unroll
+          for (int y = 0; y < RP; ++y)
+            if (x * RP + y < F) {
+              const int f = nth(x * RP + y);
+              fr[(s + 1) & 1][f] = s < 3 ? frag(slot, f, s + 1) : frag(next, f, 0);
+              if (s == 3) raw[f] = scale(next, f);
+            }
+          const uint32_t sw = sc[s >> 1][j], sa = sc[s >> 1][TN + i];
+          const i32x8 wf = operand(fr[s & 1][j]), af = operand(fr[s & 1][TN + i]);
+          acc[j][i] = s & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 2, sw, 2, sa)
+                            : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf, af, acc[j][i], 4, 4, 0, sw, 0, sa);
+          const int at = ((s + 1) & 3) * T + x;  // products behind the barrier
+          if (s == 3 ? more == 2 : more >= 1)
+#pragma unroll
+            for (int t = 0; t < PER; ++t)
+              if (issue_at(t) == at) issue_one(s == 3 ? kb + S : kb + S - 1, s == 3 ? slot : prev, t);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      slot = next;
+    };
+    int kb = kb0;
+    for (; kb + S < KB; ++kb) stage(kb, std::integral_constant<int, 2>());
+    if (kb + S == KB) stage(kb++, std::integral_constant<int, 1>());
+    for (; kb < KB; ++kb) stage(kb, std::integral_constant<int, 0>());
+  }
 
   // Epilogue, 32 rows of the wave at a time through LDS, so that its code is short (it runs once, and
   // every line of it is fetched) and its stores are whole: element e of a lane is output 8 (e / 4) + 4 kq +
@@ -423,8 +498,8 @@ struct Tile {
 };
 static const Tile tiles[] = {{256, 256, 256, 256, 8.7, 1.65, 5.3, 0.97}, {193, 192, 256, 256, 6.5, 1.40, 4.0, 0.77},
                              {192, 192, 128, 256, 5.2, 0.74, 4.2, 0.46}, {128, 128, 128, 512, 5.0, 1.05, 2.5, 0.46},
-                             {65, 64, 128, 512, 3.4, 0.63, 2.4, 0.26},   {64, 64, 64, 512, 2.8, 0.41, 2.1, 0.22},
-                             {32, 32, 64, 1024, 3.1, 0.55, 1.8, 0.21}};
+                             {65, 64, 128, 512, 3.4, 0.63, 2.4, 0.26},   {64, 64, 64, 512, 3.1, 0.38, 2.4, 0.18},
+                             {32, 32, 64, 1024, 3.4, 0.53, 2.1, 0.17}};
 static constexpr long MAX_THREADS = 1L << 32;  // a grid has fewer
 
 static long tiles_of(int M, int N, int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
