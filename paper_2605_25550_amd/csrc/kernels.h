@@ -192,7 +192,7 @@ struct LinF4Args {
   float* part;  // go to part[range][M][N rounded up to 8]
 };
 struct LinF4Plan {
-  int tile;  // 0: the kernel of few rows; an id of linear_fp4.hip's tiles; -1: it would take a grid of 2^32 threads
+  int tile;  // an id of linear_fp4.hip's tiles; -1: each would take a grid of 2^32 threads
   int split;
   size_t bytes;  // of part
 };

@@ -59,113 +59,168 @@ __device__ __forceinline__ void store_y8(const LinF4Args& a, int m, int n, const
 
 __device__ __forceinline__ i32x8 operand(u32x4 c) { return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
 
+// 4 bytes per lane from gsrc into LDS at (wave-uniform) lds_base + 4 * lane.
+__device__ __forceinline__ void dma_4(const void* gsrc, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_base), "v"(gsrc) : "memory", "m0");
+}
+
+// 4 bytes per lane from sbase + voff (sbase wave-uniform) into LDS at (wave-uniform) lds_base + 4 * lane.
+__device__ __forceinline__ void dma_4s(const void* sbase, unsigned voff, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(lds_base), "v"(voff), "s"(sbase)
+               : "memory", "m0");
+}
+
 // Scales of the eight blocks of a panel as a lane needs them: those of its quarter of 128 k (or half of
 // 64) in the low byte of each word; behind the last of `left` blocks 0, 2^-127, beside which codes are nothing.
 __device__ __forceinline__ u32x2 panel_mask(int left) {
   return u32x2{left >= 4 ? ~0u : (1u << (8 * left)) - 1u, left >= 8 ? ~0u : left <= 4 ? 0u : (1u << (8 * left - 32)) - 1u};
 }
 
-// At most 16 rows: bound by the weights' bytes, and when those are few by the launch and a chain of loads.
-// A workgroup owns 16 outputs of every row (32 where they are quantised: a block); its waves divide the
-// panels of 256 k, load fragments of v_mfma_scale_f32_16x16x128_f8f6f4 from global memory, U panels ahead,
-// and add their sums through LDS in order.  Past K a row's last bytes come again.
-template <int TN, int NW, int OUT>
+// Few rows: bound by the weights' bytes, and when those are few by the launch and a chain of loads.  A
+// workgroup owns 16 outputs (32 where they are quantised: a block) of 16 TM rows; its waves divide the
+// panels of 256 k, each with a ring of two of its own that DMA fills, so that no wave waits for another,
+// and add their sums through LDS in order.  DMA brings whole lines of eight rows an instruction, laid out as
+// the tiles' (loads of fragments, 16 rows at once, take four times as long: 16 x 18432 x 4608 21.6 us,
+// against 10.9).  Past K a row's last bytes come again.
+template <int TM, int TN, int NW, int OUT>
 __global__ __launch_bounds__(NW * 64) void linear_f4_rows_kernel(LinF4Args a) {
-  constexpr int U = 2;
+  constexpr int U = 2, F = TN + TM, R = 16 * F, PANEL = R * 136, DATA = R / 8, SC = (R + 31) / 32, PER = DATA + SC;
   static_assert(OUT != 3 || TN == 2, "a block of 32");
-  __shared__ f32x4 sum[NW][TN][64];
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[NW * U * PANEL];  // rows of W, rows of A; their scales
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
-  const int n0 = blockIdx.x * 16 * TN, panels = (a.K + 255) / 256;
+  const int n0 = blockIdx.x * 16 * TN, m0 = blockIdx.y * 16 * TM, panels = (a.K + 255) / 256;
   const long half = a.K / 2;
-  int row[TN + 1];  // of W, and the last of A
+  unsigned char* mine = ring + wave * U * PANEL;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(mine));
+
+  // instruction t: rows 8 t .. 8 t + 7 of W, then of A; of the scales: rows 32 t .. 32 t + 31
+  auto w_row = [&](int r) { return (long)min(n0 + r, a.N - 1); };
+  auto a_row = [&](int r) { return (long)min(m0 + r - 16 * TN, a.M - 1); };
+  const uint8_t *src[DATA], *sc_src[SC];
+  long sc_step[SC];
 #pragma unroll
-  for (int j = 0; j < TN; ++j) row[j] = min(n0 + j * 16 + r16, a.N - 1);
-  row[TN] = min(r16, a.M - 1);
-  f32x4 acc[TN];
+  for (int t = 0; t < DATA; ++t)
+    src[t] = t < 2 * TN ? a.w + w_row(8 * t + (lane >> 3)) * half : a.a + a_row(8 * t + (lane >> 3)) * half;
 #pragma unroll
-  for (int j = 0; j < TN; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 fr[U][TN + 1][2];
-  u32x2 sc[U][TN + 1];
-  auto load = [&](int u, int p) {
-    if (p >= panels) return;
+  for (int t = 0; t < SC; ++t) {
+    const int r = min(32 * t + (lane >> 1), R - 1);
+    sc_src[t] = (r < 16 * TN ? a.w_scale + w_row(r) * 8 : a.a_scale + a_row(r) * 8) + (lane & 1) * 4;
+    sc_step[t] = (r < 16 * TN ? a.N : a.M) * 8L;
+  }
+  auto issue = [&](int p, int u) {
+    const unsigned dst = lds0 + (unsigned)(u * PANEL);
 #pragma unroll
-    for (int f = 0; f <= TN; ++f) {
-      const uint8_t* codes = (f < TN ? a.w : a.a) + row[f] * half;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) fr[u][f][h] = *(const u32x4*)(codes + min(p * 128L + h * 64 + kq * 16, half - 16));
-      sc[u][f] = *(const u32x2*)((f < TN ? a.w_scale : a.a_scale) + ((long)p * (f < TN ? a.N : a.M) + row[f]) * 8);
+    for (int t = 0; t < DATA; ++t) {
+      const int chunk = (lane & 7) ^ ((4 * t + (lane >> 4)) & 7);
+      dma_16(src[t] + min(p * 128L + chunk * 16, half - 16), dst + (unsigned)(t * 1024));
     }
-  };
 #pragma unroll
-  for (int u = 0; u < U; ++u) load(u, wave + u * NW);
-  for (int p = wave; p < panels; p += U * NW)
+    for (int t = 0; t < SC; ++t)
+      if (32 * t + (lane >> 1) < R) dma_4(sc_src[t] + p * sc_step[t], dst + (unsigned)(R * 128 + t * 256));
+  };
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int count = (panels - wave + NW - 1) / NW;  // panels wave, wave + NW, ...
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (u < count) issue(wave + u * NW, u);
+  for (int i0 = 0; i0 < count; i0 += U)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (p + u * NW >= panels) break;
-      const u32x2 mask = panel_mask(a.K / 32 - (p + u * NW) * 8);
+      const int n = i0 + u, p = wave + n * NW;
+      if (n >= count) break;
+      if (n + U <= count) wait_vmcnt<(U - 1) * PER>();  // (the later ones may be on their way)
+      else wait_vmcnt<0>();
+      const unsigned char* at = mine + u * PANEL;
+      const u32x2 mask = panel_mask(a.K / 32 - p * 8);
+      u32x4 fr[F][2];
+      uint32_t sc[F][2];
+#pragma unroll
+      for (int f = 0; f < F; ++f) {
+        const u32x2 raw = *(const u32x2*)(at + R * 128 + (f * 16 + r16) * 8);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          fr[f][h] = *(const u32x4*)(at + (f * 16 + r16) * 128 + (((h * 4 + kq) ^ ((r16 >> 1) & 7)) << 4));
+          sc[f][h] = (raw[h] & mask[h]) >> (8 * kq);
+        }
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(fr[u][j][h]), operand(fr[u][TN][h]), acc[j], 4, 4, 0,
-                                                                    (sc[u][j][h] & mask[h]) >> (8 * kq), 0,
-                                                                    (sc[u][TN][h] & mask[h]) >> (8 * kq));
-      load(u, p + (u + U) * NW);
-    }
 #pragma unroll
-  for (int j = 0; j < TN; ++j) sum[wave][j][lane] = acc[j];
+          for (int i = 0; i < TM; ++i)
+            acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(fr[j][h]), operand(fr[TN + i][h]), acc[j][i], 4,
+                                                                         4, 0, sc[j][h], 0, sc[TN + i][h]);
+      if (n + U < count) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+        issue(p + U * NW, u);
+      }
+    }
   __syncthreads();
-  if (wave != 0) return;
-  // a lane: outputs 4 kq .. 4 kq + 3 of each 16, of row r16
-  float y[TN][4];
+  f32x4(*sum)[TN][TM][64] = (f32x4(*)[TN][TM][64])ring;
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    f32x4 t = sum[0][j][lane];
+  for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int w = 1; w < NW; ++w) t += sum[w][j][lane];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      y[j][e] = t[e];
-      if (a.bias) y[j][e] += bias_at<OUT>(a, min(n0 + j * 16 + kq * 4 + e, a.N - 1));
-      if (a.act) y[j][e] = gelu_tanh(y[j][e]);
-    }
-  }
-  const int n = n0 + kq * 4;
-  if constexpr (OUT == 3) {
-    uint32_t mx = 0u;
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) mx = max(mx, abs_bits(y[j][e]));
-    const auto p16 = __builtin_amdgcn_permlane16_swap(mx, mx, false, false);
-    mx = max(p16[0], p16[1]);
-    const auto p32 = __builtin_amdgcn_permlane32_swap(mx, mx, false, false);
-    const uint32_t s = f4_scale(max(p32[0], p32[1]));
-    if (r16 >= a.M) return;
-    const float v[8] = {y[0][0], y[0][1], y[0][2], y[0][3], y[1][0], y[1][1], y[1][2], y[1][3]};
-    const uint32_t c = pack_f4x8(v, s);
-    uint8_t* o = (uint8_t*)a.out + ((long)r16 * a.N + n) / 2;
-    *(uint16_t*)o = (uint16_t)c;
-    *(uint16_t*)(o + 8) = (uint16_t)(c >> 16);
-    if (kq == 0) store_scale(a, r16, n0, s);
-  } else {
-    if (r16 >= a.M) return;
+    for (int i = 0; i < TM; ++i) sum[wave][j][i][lane] = acc[j][i];
+  __syncthreads();
+  // a lane: outputs 4 kq .. 4 kq + 3 of each 16, of row r16 of each 16
+  for (int i = wave; i < TM; i += NW) {
+    const int m = m0 + i * 16 + r16, n = n0 + kq * 4;
+    float y[TN][4];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int nj = n + j * 16;
-      const long o = (long)r16 * a.N + nj;
-      if (nj < a.N && a.N % 4 == 0) {
-        if (OUT == 0) *(f32x4*)((float*)a.out + o) = f32x4{y[j][0], y[j][1], y[j][2], y[j][3]};
-        else *(u32x2*)((bf16_t*)a.out + o) = u32x2{pack_bf16x2(y[j][0], y[j][1]), pack_bf16x2(y[j][2], y[j][3])};
-      } else {
+      f32x4 t = sum[0][j][i][lane];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (nj + e < a.N) {
-            if (OUT == 0) ((float*)a.out)[o + e] = y[j][e];
-            else ((bf16_t*)a.out)[o + e] = f2bf(y[j][e]);
-          }
+      for (int w = 1; w < NW; ++w) t += sum[w][j][i][lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[j][e] = t[e];
+        if (a.bias) y[j][e] += bias_at<OUT>(a, min(n + j * 16 + e, a.N - 1));
+        if (a.act) y[j][e] = gelu_tanh(y[j][e]);
+      }
+    }
+    if constexpr (OUT == 3) {
+      uint32_t mx = 0u;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = max(mx, abs_bits(y[j][e]));
+      const auto p16 = __builtin_amdgcn_permlane16_swap(mx, mx, false, false);
+      mx = max(p16[0], p16[1]);
+      const auto p32 = __builtin_amdgcn_permlane32_swap(mx, mx, false, false);
+      const uint32_t s = f4_scale(max(p32[0], p32[1]));
+      if (m >= a.M) continue;
+      const float v[8] = {y[0][0], y[0][1], y[0][2], y[0][3], y[1][0], y[1][1], y[1][2], y[1][3]};
+      const uint32_t c = pack_f4x8(v, s);
+      uint8_t* o = (uint8_t*)a.out + ((long)m * a.N + n) / 2;
+      *(uint16_t*)o = (uint16_t)c;
+      *(uint16_t*)(o + 8) = (uint16_t)(c >> 16);
+      if (kq == 0) store_scale(a, m, n0, s);
+    } else {
+      if (m >= a.M) continue;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int nj = n + j * 16;
+        const long o = (long)m * a.N + nj;
+        if (nj < a.N && a.N % 4 == 0) {
+          if (OUT == 0) *(f32x4*)((float*)a.out + o) = f32x4{y[j][0], y[j][1], y[j][2], y[j][3]};
+          else *(u32x2*)((bf16_t*)a.out + o) = u32x2{pack_bf16x2(y[j][0], y[j][1]), pack_bf16x2(y[j][2], y[j][3])};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (nj + e < a.N) {
+              if (OUT == 0) ((float*)a.out)[o + e] = y[j][e];
+              else ((bf16_t*)a.out)[o + e] = f2bf(y[j][e]);
+            }
+        }
       }
     }
   }
@@ -177,14 +232,6 @@ __device__ __forceinline__ void tile_at(int tile, int tiles_m, int tiles_n, int*
   const int per = 8 * tiles_n, grp = tile / per, gm = min(8, tiles_m - grp * 8), in_grp = tile - grp * per;
   *tm = grp * 8 + in_grp % gm;
   *tn = in_grp / gm;
-}
-
-// 4 bytes per lane from sbase + voff (sbase wave-uniform) into LDS at (wave-uniform) lds_base + 4 * lane.
-__device__ __forceinline__ void dma_4s(const void* sbase, unsigned voff, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-               :
-               : "s"(lds_base), "v"(voff), "s"(sbase)
-               : "memory", "m0");
 }
 
 // Many rows: a workgroup of WM x WN waves owns BM rows x BN outputs.  Stages of 256 k (128 bytes, whole
@@ -481,25 +528,31 @@ __global__ __launch_bounds__(256) void linear_f4_join_kernel(LinF4Args a) {
   store_y8<OUT>(a, i < groups ? m : a.M, n, y);
 }
 
-// The plan of a product: at most 16 rows go to the kernel of few rows while their weights are few (16 x
-// 4608 x 1152 5.8 us against 7.5 in tiles, 16 x 8192 x 6144 10.4 in tiles against 13), else the tile with
-// the least estimate of
+// The plan of a product: the kernel of few rows (16 or 32 of them a workgroup) or the tile with the least
+// estimate of
 //   `first` us for every round of workgroups (`tail` for a last one with few) and `stage` us for each of its
 //   panels of k (`light` where there are few workgroups),
-// fitted to 480 timings (16 .. 17550 rows, K of 384 .. 8192, N of 1152 .. 6144) within 4% in the mean; the
-// tile that it picks takes 1.6% more than the best of all in the mean, 15% at most.  Measured, us, in tiles
-// of 256 x 256, 192 x 256, 192 x 128, 128 x 128, 64 x 128, 64 x 64, 32 x 64:
-//   17550 x 4608 x 4608  184  199  234  223  278          4096 x 4608 x 1152  29  25  19  21  24  26
-//   1997 x 1152 x 4608    17  14   18   17   19  25        600 x 1152 x 4608  13  11  9.9  8.6  9.0  11
-//   200 x 4608 x 1152     25  20   15   12  9.7  8.6  7.8
+// fitted to 1000 timings (1 .. 17550 rows, K of 384 .. 18432, N of 384 .. 12288); what it picks takes 0.8%
+// more than the best of all in the mean, 12% at most.  Measured, us:
+//                        256x256 192x256 192x128 128x128 64x128 64x64 32x64 32 rows 16 rows
+//   17550 x 4608 x 4608     190     208     242     230    282
+//   4096 x 4608 x 1152       31      27      20      21     25    28
+//   1997 x 1152 x 4608       17      14      19      18     19    25
+//   600 x 1152 x 4608        13      11     9.8     8.9    9.2    11    12      20
+//   77 x 1152 x 4608                                7.8    6.4   5.5   5.3     6.1     6.0
+//   77 x 4608 x 1152                                 13     10   8.0   7.9     5.0     4.8
+//   16 x 8192 x 6144                                 20     15    11    11     7.8     6.6
+// Ranges of k that are added in a second launch pay where there are few tiles and k is long: 1000 x 18432 x
+// 384 16 us in two, 19 in one.
 struct Tile {
   int id, bm, bn, slots;
   double first, stage, tail, light;
 };
-static const Tile tiles[] = {{256, 256, 256, 256, 8.7, 1.65, 5.3, 0.97}, {193, 192, 256, 256, 6.5, 1.40, 4.0, 0.77},
-                             {192, 192, 128, 256, 5.2, 0.74, 4.2, 0.46}, {128, 128, 128, 512, 5.0, 1.05, 2.5, 0.46},
-                             {65, 64, 128, 512, 3.4, 0.63, 2.4, 0.26},   {64, 64, 64, 512, 3.1, 0.38, 2.4, 0.18},
-                             {32, 32, 64, 1024, 3.4, 0.53, 2.1, 0.17}};
+static const Tile tiles[] = {{256, 256, 256, 256, 8.4, 1.68, 5.8, 0.90}, {193, 192, 256, 256, 6.5, 1.40, 4.2, 0.74},
+                             {192, 192, 128, 256, 5.4, 0.74, 4.3, 0.43}, {128, 128, 128, 512, 5.1, 1.06, 3.0, 0.41},
+                             {65, 64, 128, 512, 3.8, 0.64, 2.7, 0.25},   {64, 64, 64, 512, 3.2, 0.41, 2.3, 0.16},
+                             {32, 32, 64, 1024, 3.7, 0.50, 2.0, 0.17},   {2, 32, 16, 768, 1.56, 0.24, 1.52, 0.05},
+                             {1, 16, 16, 1024, 1.37, 0.20, 1.35, 0.04}};
 static constexpr long MAX_THREADS = 1L << 32;  // a grid has fewer
 
 static long tiles_of(int M, int N, int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
@@ -507,18 +560,20 @@ static long tiles_of(int M, int N, int bm, int bn) { return (long)((M + bm - 1) 
 LinF4Plan linear_fp4_plan(int M, int N, int K, int dtype) {
   LinF4Plan p{};
   p.split = 1;
-  const int panels = (K + 255) / 256;
-  if (M <= 16 && panels < 24) return p;
   p.tile = -1;
   double best = 0;
+  const int panels = (K + 255) / 256;
   for (const Tile& c : tiles) {
-    const long t = tiles_of(M, N, c.bm, c.bn);
-    for (int s = 1; s <= 8 && (s == 1 || (t * s <= c.slots && panels >= 4 * s)); ++s) {
+    const bool rows = c.id <= 2;
+    if (rows && M > 4096) continue;  // (their grid's second dimension)
+    const long t = tiles_of(M, N, c.bm, rows && dtype == 3 ? 32 : c.bn);
+    for (int s = 1; s <= 8 && (s == 1 || (!rows && t * s <= c.slots && panels >= 4 * s)); ++s) {
       const long wg = t * s, full = wg / c.slots, rem = wg % c.slots;
-      const double u = (double)rem / c.slots, n = (double)panels / s;
+      // (workgroups of few rows take 1.6 times as long for the 32 outputs that they quantise)
+      const double u = (double)rem / c.slots, n = (double)panels / s * (rows && dtype == 3 ? 1.6 : 1.0);
       double us = full * (c.first + n * c.stage);
       if (rem) us += c.tail + (c.first - c.tail) * u + n * (c.light + (c.stage - c.light) * u);
-      if (s > 1) us += 4.0 + 4e-6 * s * M * N;
+      if (s > 1) us += 3.0 + 2.5e-6 * s * M * N;
       if (wg * 512 >= MAX_THREADS || (p.tile > 0 && us >= best)) continue;
       best = us;
       p.tile = c.id;
@@ -529,14 +584,11 @@ LinF4Plan linear_fp4_plan(int M, int N, int K, int dtype) {
   return p;
 }
 
-template <int OUT>
+template <int TM, int OUT>
 static void launch_rows(const LinF4Args& a, hipStream_t st) {
-  // 32 outputs a workgroup where 16 would give a CU two of them and each a long chain: 16 x 4608 x 4608 7.0 us
-  // against 7.7, 16 x 1152 x 12288 4.8 against 4.5
-  const int tn = OUT == 3 || (a.N > 4096 && a.K > 2048) ? 2 : 1;
-  const dim3 grid((a.N + 16 * tn - 1) / (16 * tn)), block(256);
-  if (tn == 2) hipLaunchKernelGGL((linear_f4_rows_kernel<2, 4, OUT>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((linear_f4_rows_kernel<OUT == 3 ? 2 : 1, 4, OUT>), grid, block, 0, st, a);
+  constexpr int TN = OUT == 3 ? 2 : 1;
+  const dim3 grid((a.N + 16 * TN - 1) / (16 * TN), (a.M + 16 * TM - 1) / (16 * TM));
+  hipLaunchKernelGGL((linear_f4_rows_kernel<TM, TN, 4, OUT>), grid, dim3(256), 0, st, a);
 }
 
 template <int BM, int BN, int WM, int WN, int S, int OUT>
@@ -550,7 +602,8 @@ static void launch_tile(const LinF4Args& a, hipStream_t st) {
 
 template <int OUT>
 static void launch_out(const LinF4Args& a, int tile, hipStream_t st) {
-  if (tile == 0) launch_rows<OUT>(a, st);
+  if (tile == 1) launch_rows<1, OUT>(a, st);
+  else if (tile == 2) launch_rows<2, OUT>(a, st);
   else if (tile == 256) launch_tile<256, 256, 4, 2, 2, OUT>(a, st);
   else if (tile == 193) launch_tile<192, 256, 2, 4, 2, OUT>(a, st);
   else if (tile == 192) launch_tile<192, 128, 2, 2, 3, OUT>(a, st);

@@ -137,7 +137,7 @@ def test_two_calls_at_once():
     """Two streams, each with operands and workspaces of its own."""
     sets = []
     for n in range(2):
-        c = Linear(77, 12288, 352, dtype="fp4", seed=n)  # k divided: uses a workspace
+        c = Linear(300, 18432, 1152, dtype="fp4", seed=n)  # k divided: uses a workspace
         x = rand(50 + n, 300, 512, dtype=BF)
         q, k = rand(60 + n, 300, 6, 64, dtype=BF), rand(70 + n, 300, 2, 64, dtype=BF)
         qo, ko = torch.empty_like(q), torch.empty_like(k)
@@ -191,16 +191,16 @@ def test_refusals_on_the_device():
             dm.dequantize_fp4(args[1], args[2], args[0])
     with pytest.raises(dm.DitError):
         dm.quantize_fp4(x[:, :40].contiguous(), torch.empty(4, 20, dtype=torch.uint8, device="cuda"), scale)
-    c = Linear(40, 12288, 96)
-    out = torch.empty(40, 96, dtype=BF, device="cuda")
+    c = Linear(300, 18432, 1152)
+    out = torch.empty(300, 1152, dtype=BF, device="cuda")
     assert c.ws is not None
     with pytest.raises(dm.DitError):
         dm.linear_fp4(c.shape, c.a, c.a_scale, c.w, c.w_scale, out, None)
     with pytest.raises(dm.DitError):
         dm.linear_fp4(c.shape, c.a, c.a_scale, c.w, c.w_scale, out, c.ws[:-256])
-    for kw in (dict(bias=torch.ones(96, device="cuda")), dict(bias=torch.ones(95, dtype=BF, device="cuda"))):
+    for kw in (dict(bias=torch.ones(1152, device="cuda")), dict(bias=torch.ones(1151, dtype=BF, device="cuda"))):
         with pytest.raises(ValueError):
             dm.linear_fp4(c.shape, c.a, c.a_scale, c.w, c.w_scale, out, c.ws, **kw)
-    for args in ((c.a[:39], c.a_scale), (c.a, c.a_scale[1:]), (c.a.view(torch.int8), c.a_scale)):
+    for args in ((c.a[:299], c.a_scale), (c.a, c.a_scale[1:]), (c.a.view(torch.int8), c.a_scale)):
         with pytest.raises(ValueError):
             dm.linear_fp4(c.shape, *args, c.w, c.w_scale, out, c.ws)

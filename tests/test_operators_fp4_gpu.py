@@ -221,18 +221,18 @@ def test_linear(dtype, M, K, N, act):
     c.check(c.run())
 
 
-# shapes for each tile of many rows, the last three with k divided
+# shapes for each tile, for the kernels of few rows, and (the last two) for k divided into ranges
 @pytest.mark.parametrize("dtype", ["bf16", "f32", "fp4"])
 @pytest.mark.parametrize("M,K,N", [(8000, 96, 3456), (2100, 96, 4416), (1997, 160, 4608), (4000, 2080, 1056), (2100, 352, 3456),
                                    (700, 96, 3456), (1000, 160, 2048), (600, 608, 1152), (16, 6432, 160), (40, 8224, 96),
-                                   (201, 18432, 1056), (77, 12320, 352)])
+                                   (70, 1056, 1152), (130, 4640, 352), (33, 12320, 352), (90, 1152, 4608), (300, 18432, 1152), (1000, 18400, 320)])
 def test_every_tile(dtype, M, K, N):
     c = Linear(M, K, N, act="gelu" if dtype == "fp4" else "none", dtype=dtype, seed=K)
     c.check(c.run())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("M,K,N", [(40, 8224, 99), (130, 12320, 1), (2101, 96, 4411), (1999, 288, 3453), (1, 4096, 4100), (16, 2080, 4611)])
+@pytest.mark.parametrize("M,K,N", [(40, 8224, 99), (130, 12320, 1), (1000, 18432, 333), (2101, 96, 4411), (1999, 288, 3453), (1, 4096, 4100), (16, 2080, 4611)])
 def test_odd_widths_of_every_kind(dtype, M, K, N):
     c = Linear(M, K, N, act="gelu", dtype=dtype, seed=K)
     c.check(c.run())
@@ -292,7 +292,7 @@ def test_linear_of_no_rows():
     dm.linear_fp4(s, a, a_s, w, w_s, torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"))
 
 
-@pytest.mark.parametrize("M,K,N,dtype", [(4, 1152, 256, "fp4"), (300, 1152, 512, "bf16"), (700, 640, 576, "fp4"), (77, 12288, 352, "fp4")])
+@pytest.mark.parametrize("M,K,N,dtype", [(4, 1152, 256, "fp4"), (300, 1152, 512, "bf16"), (700, 640, 576, "fp4"), (77, 12288, 352, "fp4"), (300, 18432, 1152, "fp4")])
 def test_repeats_streams_and_graphs(M, K, N, dtype):
     c = Linear(M, K, N, act="gelu", dtype=dtype, seed=17)
     tup = lambda t: t if isinstance(t, tuple) else (t,)  # noqa: E731
