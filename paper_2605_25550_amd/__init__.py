@@ -9,6 +9,7 @@ a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional, Sequence
 
@@ -349,6 +350,7 @@ def pos_embed_2d(grid_h: int, grid_w: int, hidden: int, pos: torch.Tensor, strea
 
 # ---------------------------------------------------------------- stand-alone operators
 _DTYPE_IDS = {torch.float32: DIT_F32, torch.bfloat16: DIT_BF16, torch.float8_e4m3fn: DIT_E4M3}
+_FLOAT_IDS = {torch.float32: DIT_F32, torch.bfloat16: DIT_BF16}
 _TORCH_DTYPES = (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.uint8)  # two MXFP4 codes in a byte
 _DTYPE_NAMES = {"f32": DIT_F32, "bf16": DIT_BF16, "e4m3": DIT_E4M3, "fp4": DIT_MXFP4}
 _MASKS = {"full": 0, "causal": 1, "prefix": 2}
@@ -608,6 +610,19 @@ def qk_shape(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Option
                    (ctypes.c_int32 * 4)(*pairs), eps, *st)
 
 
+@functools.lru_cache(maxsize=1024)
+def _qk_stated(raw: bytes):
+    """What a shape struct of these bytes states: dtype, rows, head_dim, numbers of heads, elements of pos and freqs,
+    and of q, k, v and their outputs (shape, row stride, head stride)."""
+    s = QkShape.from_buffer_copy(raw)
+    q, k = (s.heads, s.head_dim), (s.kv_heads, s.head_dim)
+    return (_TORCH_DTYPES[s.dtype] if 0 <= s.dtype < 2 else None, s.rows, s.head_dim, s.heads, s.kv_heads, s.rows * max(s.axes, 0),
+            sum(s.pairs[:min(max(s.axes, 0), 4)]),
+            ((s.rows, *q), s.q_row, s.q_head), ((s.rows, *k), s.k_row, s.k_head), ((s.rows, *k), s.v_row, s.v_head),
+            ((s.q_out_rows, *q), s.q_out_row, s.q_out_head), ((s.k_out_rows, *k), s.k_out_row, s.k_out_head),
+            ((s.k_out_rows, *k), s.v_out_row, s.v_out_head))
+
+
 def qk_norm_rope(shape: QkShape, q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
                  k_out: Optional[torch.Tensor], v: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
                  w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
@@ -616,54 +631,47 @@ def qk_norm_rope(shape: QkShape, q: Optional[torch.Tensor], k: Optional[torch.Te
     """Every head of q and k normed (w_q, w_k [head_dim] fp32) and turned by its row's
     positions pos [rows, axes] int32 at freqs [pairs] fp64 into q_out and k_out, v
     copied into v_out; q_dst, k_dst [rows] int32 name the rows that they go to."""
-    s = shape
     first = q if q is not None else k
     if first is None:
         raise ValueError("q or k must be given")
-    dt, f32, i32, dev = _TORCH_DTYPES[s.dtype], torch.float32, torch.int32, first.get_device()
-    R, H, Hk, dh, kr = s.rows, s.heads, s.kv_heads, s.head_dim, s.k_out_rows
+    dt, R, dh, H, Hk, n_pos, n_freqs, sq, sk, sv, sqo, sko, svo = _qk_stated(bytes(shape))
+    f32, i32, dev = torch.float32, torch.int32, first.get_device()
     if (q is None) != (H == 0) or (k is None) != (Hk == 0):
         raise ValueError(f"the shape states {H} heads of q and {Hk} of k")
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("q and q_out, k and k_out come together")
-    kv, kv_out = (R, Hk, dh), (kr, Hk, dh)
-    _launch(dev, stream, lib().dit_qk_norm_rope, ctypes.byref(s),
-            None if q is None else _strided_ptr(q, dt, (R, H, dh), "q", s.q_row, s.q_head, dev),
-            None if k is None else _strided_ptr(k, dt, kv, "k", s.k_row, s.k_head, dev),
-            None if v is None else _strided_ptr(v, dt, kv, "v", s.v_row, s.v_head, dev),
-            None if q is None else _strided_ptr(q_out, dt, (s.q_out_rows, H, dh), "q_out", s.q_out_row, s.q_out_head, dev),
-            None if k is None else _strided_ptr(k_out, dt, kv_out, "k_out", s.k_out_row, s.k_out_head, dev),
-            None if v_out is None else _strided_ptr(v_out, dt, kv_out, "v_out", s.v_out_row, s.v_out_head, dev),
-            _arg(w_q, f32, dh, "w_q", dev), _arg(w_k, f32, dh, "w_k", dev),
-            None if pos is None else _arg(pos, i32, R * s.axes, "pos", dev),
-            None if freqs is None else _arg(freqs, torch.float64, sum(s.pairs[:s.axes]), "freqs", dev),
+
+    def at(t, stated, name):
+        return None if t is None else _strided_ptr(t, dt, stated[0], name, stated[1], stated[2], dev)
+    _launch(dev, stream, lib().dit_qk_norm_rope, ctypes.byref(shape), at(q, sq, "q"), at(k, sk, "k"), at(v, sv, "v"),
+            at(q_out, sqo, "q_out"), at(k_out, sko, "k_out"), at(v_out, svo, "v_out"), _arg(w_q, f32, dh, "w_q", dev),
+            _arg(w_k, f32, dh, "w_k", dev), _arg(pos, i32, n_pos, "pos", dev), _arg(freqs, torch.float64, n_freqs, "freqs", dev),
             _arg(q_dst, i32, R, "q_dst", dev), _arg(k_dst, i32, R, "k_dst", dev))
 
 
 def _rows_arg(x: torch.Tensor, name: str):
-    """(rows, cols, row stride) of a [rows, cols] fp32 or bf16 device tensor with contiguous columns."""
-    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda:
+    """(rows, cols, row stride, dtype id, device) of a [rows, cols] fp32 or bf16 device tensor with contiguous columns."""
+    if x.dim() != 2 or x.dtype not in _FLOAT_IDS or not x.is_cuda:
         raise ValueError(f"{name} must be a [rows, cols] float32 or bfloat16 device tensor (got {x.dtype} {tuple(x.shape)})")
-    if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
+    (R, C), (row, col) = x.shape, x.stride()
+    if col != 1 and C > 1 and R:
         raise ValueError(f"{name}'s columns must be contiguous")
-    return x.shape[0], x.shape[1], x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return R, C, row if R > 1 else C, _FLOAT_IDS[x.dtype], x.get_device()
 
 
 def quantize_fp4(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, stream=None) -> None:
     """x [rows, cols] (rows may be strided) to MXFP4: codes [rows, cols / 2] uint8, the
     even column in the lower four bits, and scales [ceil(cols / 256), rows, 8] uint8."""
-    R, C, row = _rows_arg(x, "x")
-    dev = x.get_device()
-    _launch(dev, stream, lib().dit_quantize_fp4, R, C, _DTYPE_IDS[x.dtype], x.data_ptr(), row,
-            _arg(codes, torch.uint8, R * C // 2, "codes", dev), _arg(scale, torch.uint8, -(-C // 256) * R * 8, "scale", dev))
+    R, C, row, dt, dev = _rows_arg(x, "x")
+    _launch(dev, stream, lib().dit_quantize_fp4, R, C, dt, x.data_ptr(), row, _arg(codes, torch.uint8, R * C // 2, "codes", dev),
+            _arg(scale, torch.uint8, (C + 255) // 256 * R * 8, "scale", dev))
 
 
 def dequantize_fp4(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor, stream=None) -> None:
     """The values of MXFP4 codes and scales (as quantize_fp4 writes them) into x [rows, cols]."""
-    R, C, row = _rows_arg(x, "x")
-    dev = x.get_device()
-    _launch(dev, stream, lib().dit_dequantize_fp4, R, C, _DTYPE_IDS[x.dtype], _arg(codes, torch.uint8, R * C // 2, "codes", dev),
-            _arg(scale, torch.uint8, -(-C // 256) * R * 8, "scale", dev), x.data_ptr(), row)
+    R, C, row, dt, dev = _rows_arg(x, "x")
+    _launch(dev, stream, lib().dit_dequantize_fp4, R, C, dt, _arg(codes, torch.uint8, R * C // 2, "codes", dev),
+            _arg(scale, torch.uint8, (C + 255) // 256 * R * 8, "scale", dev), x.data_ptr(), row)
 
 
 def linear_fp4_workspace(shape: LinearShape, device="cuda") -> Optional[torch.Tensor]:
