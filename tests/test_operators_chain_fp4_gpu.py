@@ -204,3 +204,34 @@ def test_refusals_on_the_device():
     for args in ((c.a[:299], c.a_scale), (c.a, c.a_scale[1:]), (c.a.view(torch.int8), c.a_scale)):
         with pytest.raises(ValueError):
             dm.linear_fp4(c.shape, *args, c.w, c.w_scale, out, c.ws)
+
+
+def test_offsets_past_32_bits():
+    """Rows of a cache, of a strided input and of a product's output that lie more than 2^31 elements on."""
+    n = (1 << 31) // 64 + 100
+    cache = torch.empty(n, 1, 64, dtype=BF, device="cuda")
+    k = rand(1, 5, 1, 64, dtype=BF)
+    at = [n - 1, 0, n - 40, n // 2, n - 2]
+    s = dm.qk_shape(None, k, None, cache, v=None, pairs=(32,))
+    pos, fr = i32([[i] for i in range(5)]), dm.rope_freqs((32,))
+    dm.qk_norm_rope(s, None, k, None, cache, pos=pos, freqs=fr, k_dst=i32(at))
+    y, tol = reference(np64(k), 1.0, "rms", (32,), "interleaved", pos.cpu().numpy(), fr.cpu().numpy(), "bf16")
+    close(np64(cache[at]), y, tol, "cache")
+    del cache
+    wide = torch.empty((1 << 31) + 4096, dtype=BF, device="cuda")
+    x = wide.as_strided((3, 4096), (1 << 30, 1))
+    for i in range(3):
+        x[i] = rand(2 + i, 4096, dtype=BF)
+    codes, scale = quantize(x)
+    back = torch.empty_like(wide).as_strided((3, 4096), (1 << 30, 1))
+    dm.dequantize_fp4(codes, scale, back)
+    want = torch.empty(3, 4096, dtype=BF, device="cuda")
+    dm.dequantize_fp4(codes, scale, want)
+    assert torch.equal(back, want)
+    del wide, back, x
+    M, N = 70000, 32768  # 32 products of 4-bit codes: exact in fp32, and rounded once
+    c = Linear.of(*quantized(rand(5, M, 32)), *quantized(rand(6, N, 32)), None)
+    out = c.run()
+    for r in (slice(0, 50), slice(65530, 65580), slice(M - 50, M)):
+        y = c.av[r] @ c.wv.T
+        close(np64(out[r]), y, 2.0 ** -8 * np.abs(y), "product")
