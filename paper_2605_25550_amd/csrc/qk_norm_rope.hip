@@ -1,5 +1,11 @@
 // Queries and keys normed for each head and turned by the row's positions, in one pass (ditmi.h:
-// dit_qk_norm_rope).
+// dit_qk_norm_rope): a head is read once and held in registers between its statistics, the rotation and
+// the store.  The angle of a pair is the same for every head of a row: a wave makes the cosines and sines
+// of its lanes' pairs once and keeps them for all the heads that it takes.
+//
+// Bound by memory: 17550 rows of 24 + 24 heads of 128 bf16 83 us, 5.2 TB/s (a copy 5.1).  Smaller calls by
+// a wave's chain of loads (4 rows 3.6 us) and, where lanes idle, by vector instructions: 3431 rows of
+// 16 + 16 heads of 72, nine lanes of sixteen at work, layer norm, 12 us (2.6 TB/s).
 #include "common.h"
 #include "kernels.h"
 

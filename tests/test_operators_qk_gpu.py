@@ -100,13 +100,15 @@ def test_heads(dtype, norm, pairing, R, H, Hk, dh):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("norm", ["rms", "layer", "none"])
 @pytest.mark.parametrize("dh,pairs,pairing", [
     (8, (4,), "halves"), (8, (1, 2), "interleaved"), (16, (3,), "interleaved"), (24, (4, 4, 4), "halves"), (40, (7, 5, 3, 1), "interleaved"),
     (128, (16, 16), "halves"), (128, (4,), "halves"), (128, (0, 33, 0), "interleaved"), (256, (64, 32, 32), "halves"),
-    (200, (100,), "halves"), (256, (40, 44, 44), "interleaved"), (72, (12, 0, 12), "halves"), (72, (), "interleaved"), (64, (0, 0), "halves")])
-def test_widths_and_parts_of_a_head(dtype, dh, pairs, pairing):
+    (200, (100,), "halves"), (256, (40, 44, 44), "interleaved"), (72, (12, 0, 12), "halves"), (72, (), "interleaved"), (64, (0, 0), "halves"), (8, (4,), "interleaved"), (16, (8,), "halves"),
+    (16, (8,), "interleaved"), (32, (16,), "halves"), (24, (12,), "interleaved"), (64, (16,), "interleaved")])
+def test_widths_and_parts_of_a_head(dtype, norm, dh, pairs, pairing):
     """Heads of every width, turned in part, with axes of no pair; nothing to turn at all."""
-    Qk(11, 5, 2, dh, dtype, "rms", pairs, pairing, v=True, seed=dh).run().check()
+    Qk(11, 5, 2, dh, dtype, norm, pairs, pairing, v=True, seed=dh).run().check()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
