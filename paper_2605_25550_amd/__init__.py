@@ -566,7 +566,8 @@ def norm_residual(shape: NormShape, x: torch.Tensor, x_out: Optional[torch.Tenso
 
 def rope_freqs(pairs: Sequence[int], theta: float = 10000.0, device="cuda") -> torch.Tensor:
     """[sum(pairs)] fp64 angles per position, theta^(-i / n) for pair i of an axis with n."""
-    return torch.cat([theta ** (-torch.arange(n, dtype=torch.float64, device=device) / max(n, 1)) for n in pairs])
+    empty = torch.empty(0, dtype=torch.float64, device=device)
+    return torch.cat([empty] + [theta ** (-torch.arange(n, dtype=torch.float64, device=device) / max(n, 1)) for n in pairs])
 
 
 def qk_shape(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],

@@ -3,17 +3,28 @@
 // the store.  The angle of a pair is the same for every head of a row: a wave makes the cosines and sines
 // of its lanes' pairs once and keeps them for all the heads that it takes.
 //
-// Bound by memory: 17550 rows of 24 + 24 heads of 128 bf16 83 us, 5.2 TB/s (a copy 5.1).  Smaller calls by
-// a wave's chain of loads (4 rows 3.6 us) and, where lanes idle, by vector instructions: 3431 rows of
-// 16 + 16 heads of 72, nine lanes of sixteen at work, layer norm, 12 us (2.6 TB/s).
+// Bound by memory: 17550 rows of 24 + 24 heads of 128 bf16 83 us, 5.2 TB/s (a copy 5.1), of 16 + 16 heads of
+// 72 34 us, 4.7 TB/s (41 with nine lanes of sixteen at work instead of seven heads in a wave).  Smaller calls
+// by a wave's chain of loads: 4 rows 3.6 us, 3431 rows of 16 + 16 heads of 72 with layer norms 11 (2.9 TB/s).
 #include "common.h"
 #include "kernels.h"
 
 namespace ditmi {
 
-// Sum over aligned groups of N lanes; every lane gets it.
+// Sum over groups of N lanes, every lane gets it: 9, or a power of two.
 template <int N>
 __device__ __forceinline__ float group_sum(float v) {
+  if constexpr (N == 9) {  // sums of 2, 4 and 8 neighbours round the group, and the ninth
+    const int lane = threadIdx.x & 63, base = lane / 9 * 9, l = lane - base;
+    auto from = [&](float x, int k) {
+      const int src = base + (l + k >= 9 ? l + k - 9 : l + k);
+      return __int_as_float(__builtin_amdgcn_ds_bpermute(src * 4, __float_as_int(x)));
+    };
+    const float ninth = from(v, 8);
+    v += from(v, 1);
+    v += from(v, 2);
+    return v + from(v, 4) + ninth;
+  }
   if (N > 1) v += dpp_move<0xB1>(v);
   if (N > 2) v += dpp_move<0x4E>(v);
   if (N > 4) v += dpp_move<0x141>(v);
@@ -62,18 +73,18 @@ struct Raw {
 };
 
 // A wave takes one of a row's segments: chunks seg, seg + segments, ... of 64 / LP heads of one tensor,
-// those of q before those of k and of v.  LP lanes (a power of two, dh / 8 of them at work) hold a head,
+// those of q before those of k and of v.  LP lanes (dh / 8 of them at work) hold a head,
 // lane l its pairs 4 l .. 4 l + 3: eight neighbours, or, where a head's halves are paired, four of each.
 // The first chunk's values are on their way while the angles are made, the next chunk's while one is
 // computed.
 template <typename T, int LP, bool HALVES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   constexpr int HPW = 64 / LP;
-  const int lane = threadIdx.x & 63, l = lane & (LP - 1), g = lane / LP;
+  const int lane = threadIdx.x & 63, g = lane / LP, l = lane - g * LP;
   const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= (long)a.rows * a.segments) return;
   const int row = (int)((unsigned)unit / (unsigned)a.segments), seg = (int)unit - row * a.segments;
-  const bool work = l < a.dh / 8;
+  const bool work = l < a.dh / 8 && g < HPW;
   const int lc = work ? l : 0;
   const bool turned = lc * 4 < a.P;  // (where halves are paired P is a multiple of four)
   const int at = HALVES && turned ? lc * 4 : 8 * lc;
@@ -161,25 +172,30 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   }
 }
 
+static int lanes_per_head(int dh) {
+  const int lanes = dh / 8;  // (nine: DiT-XL/2's head_dim of 72)
+  int lp = 1;
+  while (lp < lanes) lp *= 2;
+  return lanes == 9 ? 9 : lp;
+}
+
 template <typename T, bool HALVES>
 static void launch_qk(const QkArgs& a, hipStream_t st) {
-  const int lanes = a.dh / 8, lp = lanes <= 1 ? 1 : lanes <= 2 ? 2 : lanes <= 4 ? 4 : lanes <= 8 ? 8 : lanes <= 16 ? 16 : 32;
+  const int lp = lanes_per_head(a.dh);
   const dim3 grid((unsigned)(((long)a.rows * a.segments + 3) / 4)), block(256);
 #define QK(LP) hipLaunchKernelGGL((qk_norm_rope_kernel<T, LP, HALVES>), grid, block, 0, st, a)
   if (lp == 1) QK(1);
   else if (lp == 2) QK(2);
   else if (lp == 4) QK(4);
   else if (lp == 8) QK(8);
+  else if (lp == 9) QK(9);
   else if (lp == 16) QK(16);
   else QK(32);
 #undef QK
 }
 
 hipError_t launch_qk_norm_rope(QkArgs a, int dtype, hipStream_t st) {
-  const int lanes = a.dh / 8;
-  int lp = 1;
-  while (lp < lanes) lp *= 2;
-  const int hpw = 64 / lp, chunks = (a.H + hpw - 1) / hpw + (a.Hk + hpw - 1) / hpw + (a.Hv + hpw - 1) / hpw;
+  const int hpw = 64 / lanes_per_head(a.dh), chunks = (a.H + hpw - 1) / hpw + (a.Hk + hpw - 1) / hpw + (a.Hv + hpw - 1) / hpw;
   // four waves per SIMD, and no wave with more than six chunks: 17550 rows of 24 + 24 heads of 128 85 us in
   // two segments against 91 in one; 3431 rows of 16 + 16 of 72 14.0 in two, 18.0 in eight
   const int fill = (4096 + a.rows - 1) / a.rows, most = (chunks + 5) / 6;

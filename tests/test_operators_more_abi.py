@@ -161,3 +161,4 @@ def test_binding_refuses_before_the_library(dm):
 def test_rope_freqs(dm):
     f = dm.rope_freqs((2, 0, 4), theta=16.0, device="cpu")
     assert f.dtype == torch.float64 and torch.equal(f, torch.tensor([1.0, 0.25, 1.0, 0.5, 0.25, 0.125], dtype=torch.float64))
+    assert dm.rope_freqs((), device="cpu").shape == (0,)
