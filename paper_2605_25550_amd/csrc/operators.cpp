@@ -471,7 +471,10 @@ dit_status dit_qk_norm_rope(const dit_qk_shape* s, const void* q, const void* k,
                             const int32_t* q_dst, const int32_t* k_dst, void* stream) {
   TRY(check_qk(s));
   const int unit = s->dtype == DIT_BF16 ? 8 : 4, dh = s->head_dim, R = s->rows, H = s->heads, Hk = s->kv_heads;
-  if ((v != nullptr) != (v_out != nullptr)) return fail(DIT_ERR_INVALID_ARG, "v and v_out come together");
+  // (tensors without rows may come as NULL)
+  if ((v != nullptr) != (v_out != nullptr) && R != 0 && !(v && s->k_out_rows == 0))
+    return fail(DIT_ERR_INVALID_ARG, "v and v_out come together");
+  if (v && !v_out) v = nullptr;  // none of its rows has a place
   if (v && Hk == 0) return fail(DIT_ERR_INVALID_ARG, "v has kv_heads heads, which are none");
   if (s->norm == DIT_NORM_NONE && (w_q || w_k)) return fail(DIT_ERR_INVALID_ARG, "w_q and w_k need a norm");
   struct {

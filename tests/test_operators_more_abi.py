@@ -54,6 +54,8 @@ def test_qk_pointers(dm):
     for n in ("q", "k", "v", "q_out", "k_out", "v_out", "w_q", "w_k"):
         assert call_qk(dm, s, **{n: 100 * P + 8}) == BAD and n in dm.last_error()
     assert call_qk(dm, s, v=None) == BAD and call_qk(dm, s, v_out=None) == BAD
+    none = qk(dm, rows=0)  # tensors without rows have no memory
+    assert call_qk(dm, none, q=None, k=None, v=None) == 0 and call_qk(dm, none, v_out=None) == 0
     assert call_qk(dm, s, pos=None) == BAD and "pos" in dm.last_error()
     assert call_qk(dm, s, freqs=None) == BAD and call_qk(dm, s, freqs=P + 4) == BAD and "freqs" in dm.last_error()
     assert call_qk(dm, s, pos=P + 2) == BAD and call_qk(dm, s, q_dst=P + 1) == BAD and call_qk(dm, s, k_dst=P + 2) == BAD
