@@ -64,6 +64,7 @@ class StepWeights(ctypes.Structure):
 
 
 _LIB: Optional[ctypes.CDLL] = None
+_CALLS = None  # the compiled calls, where they were built
 
 
 class CondWeights(ctypes.Structure):
@@ -144,8 +145,23 @@ def lib() -> ctypes.CDLL:
     L.dit_last_error.argtypes = []
     L.dit_last_error.restype = ctypes.c_char_p
     L.dit_version.restype = ctypes.c_int
+    _bind_calls(L)
     _LIB = L
     return L
+
+
+def _bind_calls(L: ctypes.CDLL) -> None:
+    """The compiled calls of the operators whose small sizes the host bounds
+    (csrc/marshal.cpp), of this library; where they were not built, or for
+    another torch, the checks below make every call."""
+    global _CALLS
+    try:
+        from . import _marshal
+    except ImportError:
+        return
+    _marshal.bind(LinearShape, QkShape, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.dit_linear_fp4, L.dit_quantize_fp4, L.dit_dequantize_fp4, L.dit_qk_norm_rope)))
+    _CALLS = _marshal
 
 
 def _check(st: int) -> None:
@@ -632,6 +648,10 @@ def qk_norm_rope(shape: QkShape, q: Optional[torch.Tensor], k: Optional[torch.Te
     """Every head of q and k normed (w_q, w_k [head_dim] fp32) and turned by its row's
     positions pos [rows, axes] int32 at freqs [pairs] fp64 into q_out and k_out, v
     copied into v_out; q_dst, k_dst [rows] int32 name the rows that they go to."""
+    if stream is None and _CALLS is not None:
+        st = _CALLS.qk_norm_rope(shape, q, k, q_out, k_out, v, v_out, w_q, w_k, pos, freqs, q_dst, k_dst)
+        if st is not None:
+            return _check(st)
     first = q if q is not None else k
     if first is None:
         raise ValueError("q or k must be given")
@@ -663,6 +683,10 @@ def _rows_arg(x: torch.Tensor, name: str):
 def quantize_fp4(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, stream=None) -> None:
     """x [rows, cols] (rows may be strided) to MXFP4: codes [rows, cols / 2] uint8, the
     even column in the lower four bits, and scales [ceil(cols / 256), rows, 8] uint8."""
+    if stream is None and _CALLS is not None:
+        st = _CALLS.quantize_fp4(x, codes, scale)
+        if st is not None:
+            return _check(st)
     R, C, row, dt, dev = _rows_arg(x, "x")
     _launch(dev, stream, lib().dit_quantize_fp4, R, C, dt, x.data_ptr(), row, _arg(codes, torch.uint8, R * C // 2, "codes", dev),
             _arg(scale, torch.uint8, (C + 255) // 256 * R * 8, "scale", dev))
@@ -670,6 +694,10 @@ def quantize_fp4(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, stre
 
 def dequantize_fp4(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor, stream=None) -> None:
     """The values of MXFP4 codes and scales (as quantize_fp4 writes them) into x [rows, cols]."""
+    if stream is None and _CALLS is not None:
+        st = _CALLS.dequantize_fp4(codes, scale, x)
+        if st is not None:
+            return _check(st)
     R, C, row, dt, dev = _rows_arg(x, "x")
     _launch(dev, stream, lib().dit_dequantize_fp4, R, C, dt, _arg(codes, torch.uint8, R * C // 2, "codes", dev),
             _arg(scale, torch.uint8, (C + 255) // 256 * R * 8, "scale", dev), x.data_ptr(), row)
@@ -686,6 +714,10 @@ def linear_fp4(shape: LinearShape, a: torch.Tensor, a_scale: torch.Tensor, w: to
     """out = act(a w^T + bias) on MXFP4 codes a [rows, in / 2], w [out, in / 2] and their
     scales (quantize_fp4); bias fp32 for an fp32 output, else bf16; out [rows, out / 2]
     with out_scale [ceil(out / 256), rows, 8] for an fp4 output."""
+    if stream is None and _CALLS is not None:
+        st = _CALLS.linear_fp4(shape, a, a_scale, w, w_scale, out, workspace, bias, out_scale)
+        if st is not None:
+            return _check(st)
     s = shape
     M, K, N = s.rows, s.in_features, s.out_features
     u8, f4, dev = torch.uint8, s.dtype == DIT_MXFP4, a.get_device()

@@ -1,5 +1,6 @@
 """Build step of the HIP library: compiles csrc/ for gfx950 with hipcc into
-paper_2605_25550_amd/libditmi.so (in-tree, next to the binding)."""
+paper_2605_25550_amd/libditmi.so, and the binding's compiled calls into
+_marshal.so (in-tree, next to the binding)."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -61,7 +62,32 @@ def build(extra: list[str] | None = None, jobs: int = 8) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
     os.replace(tmp, LIB)
+    build_marshal()
     return LIB
+
+
+MARSHAL = os.path.join(PKG, "_marshal.so")
+
+
+def build_marshal() -> str:
+    """The binding's compiled calls of the operators whose small sizes the host
+    bounds (csrc/marshal.cpp, host code against torch's and Python's headers)."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    include, libs = os.path.join(base, "include"), os.path.join(base, "lib")
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
+    cmd = ["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, "-isystem", include,
+           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", os.path.join(rocm, "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL + ".tmp", "-L", libs,
+           f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for marshal.cpp:\n{r.stdout}{r.stderr}")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+    return MARSHAL
 
 
 def build_probe() -> str:
