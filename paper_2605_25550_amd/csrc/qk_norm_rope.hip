@@ -80,6 +80,9 @@ struct Raw {
 template <typename T, int LP, bool HALVES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   constexpr int HPW = 64 / LP;
+  // one of each 64 bytes of the arguments, so that their cache lines come together (1700 rows of 9 + 9 heads
+  // of 128 7.57 us against 7.73, 6862 of 16 + 16 of 72 16.9 against 17.1)
+  asm volatile("" ::"s"(a.w_q), "s"(a.rows), "s"(a.P), "s"(a.k_head), "s"(a.vo_head));
   const int lane = threadIdx.x & 63, g = lane / LP, l = lane - g * LP;
   const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= (long)a.rows * a.segments) return;
