@@ -83,12 +83,14 @@ class Struct {
 static_assert(sizeof(dit_linear_shape) == 20 && sizeof(dit_qk_shape) == 160, "the binding's structures");
 
 // The C call without the interpreter's lock, as ctypes makes it.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
 template <typename Call>
 dit_status unlocked(Call&& call) {
-  PyThreadState* state = PyEval_SaveThread();
-  const dit_status st = call();
-  PyEval_RestoreThread(state);
-  return st;
+  const Unlocked here;
+  return call();
 }
 
 int64_t panels(int64_t rows, int64_t cols) { return (cols + 255) / 256 * rows * 8; }

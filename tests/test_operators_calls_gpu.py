@@ -1,6 +1,8 @@
 """The compiled calls of queries and keys and of the 4-bit operators: they are loaded and
-take the ordinary calls, and whatever they take or leave gives what the checks in Python
-give: results, errors, streams, devices' state under capture."""
+take the ordinary calls, and what they take or leave gives what the checks in Python
+give: results, errors, on every stream and captured."""
+import threading
+
 import pytest
 import torch
 
@@ -112,6 +114,35 @@ def test_streams(path):
             assert torch.equal(graphed[n], ref[n]), n
     for n in OUTS:
         assert torch.equal(cur[n], ref[n]) and torch.equal(given[n], ref[n]), n
+
+
+def test_threads(path):
+    """Calls of several threads at once, each on a stream of its own."""
+    ref = tensors()
+    run(ref)
+    sets = [tensors() for _ in range(4)]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(t):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    run(t)
+                with pytest.raises(ValueError, match="elements"):
+                    dm.quantize_fp4(t["x"], t["x_codes"][1:], t["x_scale"])
+        except BaseException as e:  # noqa: BLE001  (reported by the test's own thread)
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(t,)) for t in sets]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join(60)
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for t in sets:
+        for n in OUTS:
+            assert torch.equal(t[n], ref[n]), n
 
 
 def test_strides_that_no_element_uses(path):
