@@ -445,7 +445,7 @@ typedef struct {
   int64_t q_out_row, q_out_head, k_out_row, k_out_head, v_out_row, v_out_head;
 } dit_qk_shape;
 
-/*   v, v_out   both or neither
+/*   v, v_out   both or neither (one without rows may be NULL beside the other)
  *   w_q, w_k   [head_dim] fp32 or NULL (ones)
  *   pos        [rows, axes] int32;  freqs [P] fp64 (both NULL without pairs)
  *   q_dst, k_dst   [rows] int32 or NULL */
