@@ -212,6 +212,7 @@ struct QkArgs {
   float eps;
   long q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head, vo_row, vo_head;
 };
+int qk_segments(int rows, int dh, int H, int Hk, int Hv);  // waves that share a row
 
 // ------------------------------------------------------------------ launchers
 // Each returns hipSuccess or the launch error.  dtype: 0 = fp32, 1 = bf16.

@@ -108,7 +108,7 @@ dit_status check_qk(const dit_qk_shape* s) {
   if (s->rows < 0 || s->heads < 0 || s->kv_heads < 0 || s->heads + (long)s->kv_heads < 1 || s->q_out_rows < 0 || s->k_out_rows < 0)
     return fail(DIT_ERR_INVALID_ARG, "rows (%d), heads (%d), kv_heads (%d), q_out_rows (%d), k_out_rows (%d) must be >= 0, one head at least",
                 s->rows, s->heads, s->kv_heads, s->q_out_rows, s->k_out_rows);
-  // (a grid has fewer than 2^32 threads: 64 for a row)
+  // (qk_segments() keeps a grid of so many rows below 2^32 threads)
   if (s->heads > 65535 || s->kv_heads > 65535 || s->rows > (1 << 24))
     return fail(DIT_ERR_UNSUPPORTED, "more than 65535 heads or 2^24 rows (%d)", s->rows);
   if (s->head_dim < 8 || s->head_dim % 8 != 0 || s->head_dim > 256)

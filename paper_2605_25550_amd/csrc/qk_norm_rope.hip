@@ -197,12 +197,19 @@ static void launch_qk(const QkArgs& a, hipStream_t st) {
 #undef QK
 }
 
-hipError_t launch_qk_norm_rope(QkArgs a, int dtype, hipStream_t st) {
-  const int hpw = 64 / lanes_per_head(a.dh), chunks = (a.H + hpw - 1) / hpw + (a.Hk + hpw - 1) / hpw + (a.Hv + hpw - 1) / hpw;
+int qk_segments(int rows, int dh, int H, int Hk, int Hv) {
+  const int hpw = 64 / lanes_per_head(dh), chunks = (H + hpw - 1) / hpw + (Hk + hpw - 1) / hpw + (Hv + hpw - 1) / hpw;
   // four waves per SIMD, and no wave with more than six chunks: 17550 rows of 24 + 24 heads of 128 85 us in
   // two segments against 91 in one; 3431 rows of 16 + 16 of 72 14.0 in two, 18.0 in eight
-  const int fill = (4096 + a.rows - 1) / a.rows, most = (chunks + 5) / 6;
-  a.segments = fill > chunks ? chunks : fill > most ? fill : most;
+  const int fill = (4096 + rows - 1) / rows, most = (chunks + 5) / 6;
+  const int want = fill > chunks ? chunks : fill > most ? fill : most;
+  // (a grid has fewer than 2^32 threads, 64 for a segment in workgroups of four: 2^24 rows leave three)
+  const int room = ((1 << 26) - 4) / rows;
+  return want < room ? want : room;
+}
+
+hipError_t launch_qk_norm_rope(QkArgs a, int dtype, hipStream_t st) {
+  a.segments = qk_segments(a.rows, a.dh, a.H, a.Hk, a.Hv);
   if (dtype == 0) a.halves ? launch_qk<float, true>(a, st) : launch_qk<float, false>(a, st);
   else a.halves ? launch_qk<bf16_t, true>(a, st) : launch_qk<bf16_t, false>(a, st);
   return hipGetLastError();
