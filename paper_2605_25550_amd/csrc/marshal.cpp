@@ -9,7 +9,10 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
+
 #include "ditmi.h"
+#include "unlocked.h"
 
 namespace {
 
@@ -22,7 +25,8 @@ struct Library {
   PyObject *linear_shape, *qk_shape;
 } lib;
 
-// What does not fit ends the function; guarded() makes None of it.
+// What does not fit ends the function; unlocked_call() makes None of it (and of torch's own exceptions, of a tensor
+// without memory).
 struct Unfit {};
 void need(bool ok) {
   if (!ok) throw Unfit();
@@ -62,36 +66,21 @@ struct Tensors {
   }
 };
 
-// The memory of a ctypes structure of that type.
+// What a ctypes structure of that type holds.
 template <typename S>
-class Struct {
-  Py_buffer view{};
-
- public:
-  Struct(PyObject* o, PyObject* type) {
-    need(lib.linear_fp4 && (PyObject*)Py_TYPE(o) == type);
-    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) {
-      PyErr_Clear();
-      throw Unfit();
-    }
+S structure(PyObject* o, PyObject* type) {
+  need(lib.linear_fp4 && (PyObject*)Py_TYPE(o) == type);
+  Py_buffer view;
+  if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) {
+    PyErr_Clear();
+    throw Unfit();
   }
-  ~Struct() { PyBuffer_Release(&view); }
-  Struct(const Struct&) = delete;
-  const S* operator->() const { return (const S*)view.buf; }
-  operator const S*() const { return (const S*)view.buf; }
-};
-static_assert(sizeof(dit_linear_shape) == 20 && sizeof(dit_qk_shape) == 160, "the binding's structures");
-
-// The C call without the interpreter's lock, as ctypes makes it.
-struct Unlocked {
-  PyThreadState* state = PyEval_SaveThread();
-  ~Unlocked() { PyEval_RestoreThread(state); }
-};
-template <typename Call>
-dit_status unlocked(Call&& call) {
-  const Unlocked here;
-  return call();
+  S s;
+  std::memcpy(&s, view.buf, sizeof(S));
+  PyBuffer_Release(&view);
+  return s;
 }
+static_assert(sizeof(dit_linear_shape) == 20 && sizeof(dit_qk_shape) == 160, "the binding's structures");
 
 int64_t panels(int64_t rows, int64_t cols) { return (cols + 255) / 256 * rows * 8; }
 
@@ -101,20 +90,20 @@ at::ScalarType float_type(int32_t dtype) {
 }
 
 // (shape, a, a_scale, w, w_scale, out, workspace, bias, out_scale)
-dit_status linear_fp4(PyObject* const* v, Py_ssize_t n) {
+auto linear_fp4(PyObject* const* v, Py_ssize_t n) {
   need(n == 9);
-  const Struct<dit_linear_shape> s(v[0], lib.linear_shape);
-  const int64_t M = s->rows, K = s->in, N = s->out;
+  const auto s = structure<dit_linear_shape>(v[0], lib.linear_shape);
+  const int64_t M = s.rows, K = s.in, N = s.out;
   need(M >= 0 && K >= 0 && N >= 0);
-  const bool f4 = s->dtype == DIT_MXFP4;
-  const at::ScalarType type = f4 ? at::kByte : float_type(s->dtype);
+  const bool f4 = s.dtype == DIT_MXFP4;
+  const at::ScalarType type = f4 ? at::kByte : float_type(s.dtype);
   Tensors c;
   void* a = c.flat(v[1], at::kByte, M * K / 2);
   void* a_scale = c.flat(v[2], at::kByte, panels(M, K));
   void* w = c.flat(v[3], at::kByte, N * K / 2);
   void* w_scale = c.flat(v[4], at::kByte, panels(N, K));
   void* out = c.flat(v[5], type, f4 ? M * N / 2 : M * N);
-  void* bias = c.flat(v[7], s->dtype == DIT_F32 ? at::kFloat : at::kBFloat16, N);
+  void* bias = c.flat(v[7], s.dtype == DIT_F32 ? at::kFloat : at::kBFloat16, N);
   void* out_scale = c.flat(v[8], at::kByte, panels(M, N));
   void* space = nullptr;
   size_t bytes = 0;
@@ -124,7 +113,7 @@ dit_status linear_fp4(PyObject* const* v, Py_ssize_t n) {
     space = t.data_ptr(), bytes = t.nbytes();
   }
   void* stream = c.stream();
-  return unlocked([&] { return lib.linear_fp4(s, a, a_scale, w, w_scale, bias, out, out_scale, space, bytes, stream); });
+  return [=] { return lib.linear_fp4(&s, a, a_scale, w, w_scale, bias, out, out_scale, space, bytes, stream); };
 }
 
 // [rows, cols] fp32 or bf16 with contiguous columns
@@ -143,63 +132,53 @@ struct Rows {
 };
 
 // (x, codes, scale)
-dit_status quantize_fp4(PyObject* const* v, Py_ssize_t n) {
+auto quantize_fp4(PyObject* const* v, Py_ssize_t n) {
   need(n == 3 && lib.quantize_fp4);
   Tensors c;
   const Rows x(c, v[0]);
   void* codes = c.flat(v[1], at::kByte, x.rows * x.cols / 2);
   void* scale = c.flat(v[2], at::kByte, panels(x.rows, x.cols));
   void* stream = c.stream();
-  return unlocked([&] { return lib.quantize_fp4((int32_t)x.rows, (int32_t)x.cols, x.dtype, x.p, x.row, codes, scale, stream); });
+  return [=] { return lib.quantize_fp4((int32_t)x.rows, (int32_t)x.cols, x.dtype, x.p, x.row, codes, scale, stream); };
 }
 
 // (codes, scale, x)
-dit_status dequantize_fp4(PyObject* const* v, Py_ssize_t n) {
+auto dequantize_fp4(PyObject* const* v, Py_ssize_t n) {
   need(n == 3 && lib.dequantize_fp4);
   Tensors c;
   const Rows x(c, v[2]);
   void* codes = c.flat(v[0], at::kByte, x.rows * x.cols / 2);
   void* scale = c.flat(v[1], at::kByte, panels(x.rows, x.cols));
   void* stream = c.stream();
-  return unlocked([&] { return lib.dequantize_fp4((int32_t)x.rows, (int32_t)x.cols, x.dtype, codes, scale, x.p, x.row, stream); });
+  return [=] { return lib.dequantize_fp4((int32_t)x.rows, (int32_t)x.cols, x.dtype, codes, scale, x.p, x.row, stream); };
 }
 
 // (shape, q, k, q_out, k_out, v, v_out, w_q, w_k, pos, freqs, q_dst, k_dst)
-dit_status qk_norm_rope(PyObject* const* v, Py_ssize_t n) {
+auto qk_norm_rope(PyObject* const* v, Py_ssize_t n) {
   need(n == 13);
-  const Struct<dit_qk_shape> s(v[0], lib.qk_shape);
-  const at::ScalarType type = float_type(s->dtype);
-  const int64_t R = s->rows, H = s->heads, Hk = s->kv_heads, dh = s->head_dim;
-  need(s->axes >= 0 && s->axes <= 4);
+  const auto s = structure<dit_qk_shape>(v[0], lib.qk_shape);
+  const at::ScalarType type = float_type(s.dtype);
+  const int64_t R = s.rows, H = s.heads, Hk = s.kv_heads, dh = s.head_dim;
+  need(s.axes >= 0 && s.axes <= 4);
   int64_t pairs = 0;
-  for (int i = 0; i < s->axes; ++i) pairs += s->pairs[i];
+  for (int i = 0; i < s.axes; ++i) pairs += s.pairs[i];
   need((v[1] != Py_None) == (H != 0) && (v[3] != Py_None) == (H != 0));
   need((v[2] != Py_None) == (Hk != 0) && (v[4] != Py_None) == (Hk != 0));
   Tensors c;
-  void* q = c.heads(v[1], type, R, H, dh, s->q_row, s->q_head);
-  void* k = c.heads(v[2], type, R, Hk, dh, s->k_row, s->k_head);
-  void* q_out = c.heads(v[3], type, s->q_out_rows, H, dh, s->q_out_row, s->q_out_head);
-  void* k_out = c.heads(v[4], type, s->k_out_rows, Hk, dh, s->k_out_row, s->k_out_head);
-  void* x = c.heads(v[5], type, R, Hk, dh, s->v_row, s->v_head);
-  void* x_out = c.heads(v[6], type, s->k_out_rows, Hk, dh, s->v_out_row, s->v_out_head);
+  void* q = c.heads(v[1], type, R, H, dh, s.q_row, s.q_head);
+  void* k = c.heads(v[2], type, R, Hk, dh, s.k_row, s.k_head);
+  void* q_out = c.heads(v[3], type, s.q_out_rows, H, dh, s.q_out_row, s.q_out_head);
+  void* k_out = c.heads(v[4], type, s.k_out_rows, Hk, dh, s.k_out_row, s.k_out_head);
+  void* x = c.heads(v[5], type, R, Hk, dh, s.v_row, s.v_head);
+  void* x_out = c.heads(v[6], type, s.k_out_rows, Hk, dh, s.v_out_row, s.v_out_head);
   const float* w_q = (const float*)c.flat(v[7], at::kFloat, dh);
   const float* w_k = (const float*)c.flat(v[8], at::kFloat, dh);
-  const int32_t* pos = (const int32_t*)c.flat(v[9], at::kInt, R * s->axes);
+  const int32_t* pos = (const int32_t*)c.flat(v[9], at::kInt, R * s.axes);
   const double* freqs = (const double*)c.flat(v[10], at::kDouble, pairs);
   const int32_t* q_dst = (const int32_t*)c.flat(v[11], at::kInt, R);
   const int32_t* k_dst = (const int32_t*)c.flat(v[12], at::kInt, R);
   void* stream = c.stream();
-  return unlocked([&] { return lib.qk_norm_rope(s, q, k, x, q_out, k_out, x_out, w_q, w_k, pos, freqs, q_dst, k_dst, stream); });
-}
-
-// The status of the C call, or None (torch's own exceptions, of a tensor without memory, are no fit either).
-template <dit_status (*call)(PyObject* const*, Py_ssize_t)>
-PyObject* guarded(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  try {
-    return PyLong_FromLong(call(v, n));
-  } catch (...) {
-    Py_RETURN_NONE;
-  }
+  return [=] { return lib.qk_norm_rope(&s, q, k, x, q_out, k_out, x_out, w_q, w_k, pos, freqs, q_dst, k_dst, stream); };
 }
 
 // bind(LinearShape, QkShape, addresses of dit_linear_fp4, dit_quantize_fp4, dit_dequantize_fp4, dit_qk_norm_rope)
@@ -219,10 +198,10 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 
 #define FUNCTION(name, fn) {name, (PyCFunction)(void*)fn, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FUNCTION("bind", bind),
-                         FUNCTION("linear_fp4", guarded<linear_fp4>),
-                         FUNCTION("quantize_fp4", guarded<quantize_fp4>),
-                         FUNCTION("dequantize_fp4", guarded<dequantize_fp4>),
-                         FUNCTION("qk_norm_rope", guarded<qk_norm_rope>),
+                         FUNCTION("linear_fp4", unlocked_call<linear_fp4>),
+                         FUNCTION("quantize_fp4", unlocked_call<quantize_fp4>),
+                         FUNCTION("dequantize_fp4", unlocked_call<dequantize_fp4>),
+                         FUNCTION("qk_norm_rope", unlocked_call<qk_norm_rope>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 
