@@ -159,6 +159,9 @@ def _bind_calls(L: ctypes.CDLL) -> None:
         from . import _marshal
     except ImportError:
         return
+    from .build import marshal_target
+    if getattr(_marshal, "BUILT_FOR", None) != marshal_target():
+        return
     _marshal.bind(LinearShape, QkShape, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.dit_linear_fp4, L.dit_quantize_fp4, L.dit_dequantize_fp4, L.dit_qk_norm_rope)))
     _CALLS = _marshal

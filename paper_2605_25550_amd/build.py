@@ -69,6 +69,13 @@ def build(extra: list[str] | None = None, jobs: int = 8) -> str:
 MARSHAL = os.path.join(PKG, "_marshal.so")
 
 
+def marshal_target() -> str:
+    """The torch and the Python that the compiled calls read tensors of: they are of
+    no use to another, whose objects may be laid out otherwise."""
+    import torch
+    return f"torch {torch.__version__} {torch.version.git_version}, Python {sys.hexversion:#x}"
+
+
 def build_marshal() -> str:
     """The binding's compiled calls of the operators whose small sizes the host
     bounds (csrc/marshal.cpp, host code against torch's and Python's headers)."""
@@ -79,7 +86,7 @@ def build_marshal() -> str:
     include, libs = os.path.join(base, "include"), os.path.join(base, "lib")
     rocm = os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
     cmd = ["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, "-isystem", include,
+           f'-DDITMI_BUILT_FOR="{marshal_target()}"', f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE, "-isystem", include,
            "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", os.path.join(rocm, "include"),
            "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL + ".tmp", "-L", libs,
            f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]

@@ -207,4 +207,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
+// BUILT_FOR: whose tensors the code above reads; the binding uses it beside no other torch or Python
+PyMODINIT_FUNC PyInit__marshal(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "BUILT_FOR", DITMI_BUILT_FOR) != 0) Py_CLEAR(m);
+  return m;
+}
