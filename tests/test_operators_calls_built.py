@@ -1,4 +1,5 @@
 """CPU tests of when the compiled calls are used: beside the torch and Python that they were built for, and no other."""
+import subprocess
 import sys
 
 import pytest
@@ -58,3 +59,25 @@ def test_another_torchs_version(calls, monkeypatch):
     monkeypatch.setattr(torch, "__version__", "2.99.0")
     dm._bind_calls(dm.lib())
     assert dm._CALLS is None
+
+
+@pytest.mark.parametrize("how", ["no compiler", "no headers"])
+def test_a_build_without_them(monkeypatch, tmp_path, how):
+    """The library is built all the same, and no module of an earlier build stays beside it."""
+    lib, old = tmp_path / "lib.so", tmp_path / "_marshal.so"
+    old.write_bytes(b"of an earlier build")
+    real = subprocess.run
+
+    def run(cmd, **kw):
+        if cmd[0] == "g++":
+            if how == "no compiler":
+                raise FileNotFoundError(2, "No such file or directory: 'g++'")
+            return real([sys.executable, "-c", "raise SystemExit('Python.h: No such file')"], **kw)
+        (tmp_path / "lib.so.tmp").write_bytes(b"linked")
+        return real([sys.executable, "-c", ""], **kw)
+    for name, value in (("SOURCES", []), ("OBJDIR", str(tmp_path)), ("LIB", str(lib)), ("MARSHAL", str(old))):
+        monkeypatch.setattr(B, name, value)
+    monkeypatch.setattr(B.subprocess, "run", run)
+    with pytest.warns(UserWarning, match="(?s)compiled calls were not built.*No such file"):
+        assert B.build() == str(lib)
+    assert lib.read_bytes() == b"linked" and not old.exists()
