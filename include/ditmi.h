@@ -261,7 +261,7 @@ dit_status dit_pos_embed_2d(int32_t grid_h, int32_t grid_w, int32_t hidden, floa
  * What the host cannot see (the int32 index arrays on the device) is bounded
  * by the kernels: an entry out of range is clamped into it, so such a call
  * computes something useless but stays inside the tensors.  Outputs must not
- * overlap inputs unless said otherwise.
+ * overlap inputs unless said otherwise, nor one another.
  * ------------------------------------------------------------------------ */
 
 /* Masked attention over documents (requests, samples): packed one behind the
@@ -412,19 +412,21 @@ dit_status dit_norm_residual(const dit_norm_shape *s, const float *x, float *x_o
  * of a video; one axis of text).  For row r, head h and x = q or k:
  *   n = norm(x) * w                     (DIT_NORM_LAYER, DIT_NORM_RMS with eps, as
  *                                       dit_norm_residual, over head_dim; or NONE)
- *   t = pos[r, axis of p] * freqs[p]    (radians, in 64 bits)
+ *   t = pos[r, axis of p] * freqs[p]    (radians; reduced to one turn in 64 bits)
  *   (n_a, n_b) = (n_a cos t - n_b sin t, n_a sin t + n_b cos t)    for pair p
  * Pair p are the elements (2p, 2p + 1) with DIT_PAIR_NEIGHBOURS and (p, p + P) with
  * DIT_PAIR_HALVES, P the number of all pairs; the first pairs[0] belong to axis 0,
  * the next pairs[1] to axis 1 and so on.  Elements from 2P on are not turned.
- * Statistics, weights and rotation in fp32, one rounding at the end; the squares of
- * a head must not overflow fp32.
+ * Statistics, weights and rotation in fp32 (for DIT_BF16 with cosines and sines that
+ * are off by 2^-18 at most), one rounding at the end; the squares of a head must not
+ * overflow fp32.
  * Row r of q goes to row q_dst[r] of q_out (r itself without q_dst), row r of k and
  * of v, which is copied as it is, to row k_dst[r] of k_out and v_out: the rooms of
  * a cache, or a joint sequence.  A row whose destination lies outside of the output
  * is not written; of two rows with one destination either's pieces may stay.  Other
  * rows of the outputs are left as they were.  q_out may be q itself (k_out k, v_out
- * v), with the same strides and without q_dst (k_dst).
+ * v), with the same strides and without q_dst (k_dst); an output that shares some
+ * elements with a tensor at another offset is one that overlaps it, and is not refused.
  *   rows >= 0 (at most 2^24);  heads, kv_heads >= 0 (either may be 0: then its
  *              tensors are not read and may be NULL);  head_dim a multiple of 8 in
  *              8 .. 256
@@ -465,7 +467,7 @@ dit_status dit_qk_norm_rope(const dit_qk_shape *s, const void *q, const void *k,
  *   scale  [ceil(cols / 256), rows, 8] bytes e + 127 (e8m0), contiguous: block b of
  *          row r at [b / 8, r, b % 8], so that what a tile of a product reads at
  *          once lies together; 0 behind the last column
- *   cols   a multiple of 32, x_row of 8;  rows >= 0 */
+ *   cols   a multiple of 32;  x_row a multiple of 8, >= cols;  rows >= 0 */
 dit_status dit_quantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const void *x, int64_t x_row, void *codes, void *scale,
                             void *stream);
 

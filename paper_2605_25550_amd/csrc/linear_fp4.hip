@@ -244,7 +244,10 @@ __device__ __forceinline__ void tile_at(int tile, int tiles_m, int tiles_n, int*
 // Bound by power when it runs long: 17550 x 18432 x 4608 654 us, 4.6 PFLOP/s, and 489 us on codes of zero.
 // Beside that a 256 x 256 tile's panel takes 2048 cycles of products, 1300 of the CU's address unit for its
 // DMA, and some 2100 for its 68 KB from the L2.  Short ones: 4096 x 4608 x 1152 18 us, of which 11 are 18
-// panels and the rest the launch, the first loads and the epilogue.
+// panels and the rest the launch, the first loads and the epilogue.  Many rows over short k by what every round
+// of workgroups costs beside its panels, for one workgroup fills a CU's LDS and nothing runs beside its first
+// loads and its epilogue: 17550 x 1152 x 4608 93 us, 2.0 PFLOP/s (89 and, with GELU, 109 into 4 bits, 120 into
+// fp32), 17550 x 3072 x 9216 281 us, 3.5 PFLOP/s.
 template <int BM, int BN, int WM, int WN, int S, int OUT>
 __global__ __launch_bounds__(WM * WN * 64) void linear_f4_tile_kernel(LinF4Args a) {
   constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, T = TM * TN, F = TN + TM;
@@ -548,6 +551,9 @@ __global__ __launch_bounds__(256) void linear_f4_join_kernel(LinF4Args a) {
 //   16 x 8192 x 6144                                 20     15    11    11     7.8     6.6
 // Ranges of k that are added in a second launch pay where there are few tiles and k is long: 1000 x 18432 x
 // 384 16 us in two, 19 in one.
+// `slots` went into the fit as workgroups of a round and are what LDS admits but for three kernels, of which it
+// admits fewer: 32 x 64 (768 workgroups), and those of few rows that quantise (768 of 16 rows, 512 of 32).  The
+// other constants are fitted to the slots as they stand.
 struct Tile {
   int id, bm, bn, slots;
   double first, stage, tail, light;
