@@ -427,9 +427,9 @@ dit_status dit_norm_residual(const dit_norm_shape *s, const float *x, float *x_o
  * rows of the outputs are left as they were.  q_out may be q itself (k_out k, v_out
  * v), with the same strides and without q_dst (k_dst); an output that shares some
  * elements with a tensor at another offset is one that overlaps it, and is not refused.
- *   rows >= 0 (at most 2^24);  heads, kv_heads >= 0 (either may be 0: then its
- *              tensors are not read and may be NULL);  head_dim a multiple of 8 in
- *              8 .. 256
+ *   rows >= 0 (at most 2^24);  heads, kv_heads >= 0 (at most 65535; either may be
+ *              0: then its tensors are not read and may be NULL);  head_dim a
+ *              multiple of 8 in 8 .. 256
  *   q_out_rows, k_out_rows   rows of q_out; of k_out and v_out
  *   dtype      of q, k, v and the outputs: DIT_F32 or DIT_BF16
  *   axes       0 .. 4;  pairs of each, together at most head_dim / 2 (a multiple of
@@ -467,7 +467,8 @@ dit_status dit_qk_norm_rope(const dit_qk_shape *s, const void *q, const void *k,
  *   scale  [ceil(cols / 256), rows, 8] bytes e + 127 (e8m0), contiguous: block b of
  *          row r at [b / 8, r, b % 8], so that what a tile of a product reads at
  *          once lies together; 0 behind the last column
- *   cols   a multiple of 32;  x_row a multiple of 8, >= cols;  rows >= 0 */
+ *   cols   a multiple of 32 (at most 2^30);  x_row a multiple of 8, >= cols (at most
+ *          2^40);  rows >= 0, fewer than 2^24 pieces of 8 rows of 256 columns */
 dit_status dit_quantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const void *x, int64_t x_row, void *codes, void *scale,
                             void *stream);
 
@@ -479,7 +480,8 @@ dit_status dit_dequantize_fp4(int32_t rows, int32_t cols, int32_t dtype, const v
 /* A linear layer on such operands:
  *   y[m, n] = act(sum_k a[m, k] a_scale[m, k/32] * w[n, k] w_scale[n, k/32] + bias[n])
  * with products and their sums in fp32 on the 4-bit matrix pipe.
- *   rows >= 0, in a multiple of 32, out >= 1
+ *   rows >= 0 (at most 2^26), in a multiple of 32 (at most 2^22), out >= 1 (at most
+ *          2^26), and a grid of fewer than 2^32 threads
  *   act    as dit_linear_fp8
  *   dtype  of out: DIT_F32, DIT_BF16, or DIT_MXFP4, which quantises every row of y
  *          anew (as dit_quantize_fp4) into out and out_scale; out a multiple of 32 */

@@ -35,38 +35,43 @@ class Plan4(ctypes.Structure):
     _fields_ = [("tile", ctypes.c_int), ("split", ctypes.c_int), ("bytes", ctypes.c_size_t)]
 
 
-@pytest.fixture(scope="module")
-def plan4():
+def plan4(M, K, N, dtype=1):
     fn = dm.lib()._ZN5ditmi15linear_fp4_planEiiii
     fn.restype, fn.argtypes = Plan4, [ctypes.c_int] * 4
-    return fn
+    return fn(M, N, K, dtype)
 
 
-# slots of each tile's ring (of the kernels of few rows: panels that four waves hold)
-RING = {256: 2, 193: 2, 192: 3, 128: 2, 65: 3, 64: 4, 32: 4, 2: 8, 1: 8}
-# (rows, in, out, tile, ranges of k): every tile's loop in its steady state, behind it its last stages and a panel in
-# part, for odd and even numbers of panels; and ranges of k of unequal lengths
-LOOPS = [(8000, 1120, 3456, 256, 1), (8000, 1440, 3456, 256, 1), (2100, 1120, 4416, 193, 1), (2100, 1440, 4416, 193, 1),
-         (4000, 2080, 1056, 192, 1), (904, 1312, 5824, 192, 1), (2100, 1376, 3456, 128, 1), (2100, 1120, 3456, 128, 1),
-         (700, 1120, 3456, 65, 1), (700, 1376, 3456, 65, 1), (1000, 2080, 2048, 64, 1), (1000, 1824, 2048, 64, 1),
-         (6922, 1696, 32, 64, 1), (4112, 1696, 32, 32, 1), (4112, 1888, 32, 32, 1), (4112, 2144, 32, 32, 1),
-         (300, 4640, 1152, 2, 1), (130, 8224, 1152, 1, 1), (1957, 58656, 1536, 256, 5), (1798, 56000, 1696, 193, 3),
-         (1110, 32320, 1184, 192, 4), (1023, 56448, 1312, 128, 5), (1097, 27072, 608, 65, 4), (4130, 9888, 32, 64, 4),
-         (66, 17504, 5824, 32, 3)]
+def loops():
+    """(rows, in, out, tile, ranges of k): for every kernel that the plan picks, whole k and divided, and for odd and even
+    numbers of panels, the smallest and the largest product of these whose workgroups take seven panels of 256 k at least (the kernels of few
+    rows, whose four waves share them, 33), the last one in part: their loops are in the steady state, rings are filled again
+    and run empty."""
+    found = {}
+    for M in (66, 130, 300, 700, 904, 1023, 1110, 1957, 2100, 4000, 4130, 6922, 8000):
+        for K in (1632, 1888, 2080, 3168, 8224, 8480, 9888, 17504, 18400, 27072, 32320, 56448, 58656):
+            for N in (32, 320, 608, 1056, 1152, 1312, 1536, 2048, 3456, 4416, 5824):
+                p, panels = plan4(M, K, N), -(-K // 256)
+                if panels // p.split < (33 if p.tile <= 2 else 7) or (M + N) * K > 2.2e8 or M * K * N > 2e11:
+                    continue
+                found.setdefault((p.tile, p.split > 1, panels % 2), []).append((M * K * N, (M, K, N, p.tile, p.split)))
+    return sorted({pick(found[k])[1] for k in found for pick in (min, max)}, key=lambda c: c[3:] + c[:3])
 
 
-@pytest.mark.parametrize("dtype", [0, 1, 3])
-@pytest.mark.parametrize("M,K,N,tile,split", LOOPS)
-def test_shapes_take_the_tiles_that_they_test(plan4, dtype, M, K, N, tile, split):
-    p = plan4(M, N, K, dtype)
-    assert (p.tile, p.split) == (tile, split)
-    assert -(-K // 256) // split > RING[tile] + 1 and K % 256
-    assert p.bytes == (split * M * N * 4 if split > 1 else 0)
+LOOPS = loops()
 
 
-def test_every_tile_is_tested():
-    assert {c[3] for c in LOOPS} == set(RING)
-    assert {c[3] for c in LOOPS if c[4] > 1} == {t for t in RING if t > 2}  # (the others divide no k)
-    for t in RING:
-        if t > 2:  # both parities
-            assert {-(-c[1] // 256) % 2 for c in LOOPS if c[3] == t and c[4] == 1} == {0, 1}, t
+def test_every_kernel_is_among_them():
+    """Whatever the plan picks for ordinary products is one that the loops' tests run, divided too where it divides."""
+    picked = set()
+    for M in (1, 8, 16, 33, 77, 200, 300, 600, 1000, 1997, 4096, 8192, 17550):
+        for K in (96, 1152, 4608, 8192, 18432):
+            for N in (1, 96, 384, 1152, 3456, 4608, 9216):
+                for dtype in (0, 1, 3):
+                    p = plan4(M, K, -(-N // 32) * 32 if dtype == 3 else N, dtype)
+                    picked.add((p.tile, p.split > 1))
+                    assert p.bytes == (p.split * M * ((-(-N // 32) * 32 if dtype == 3 else N) + 7 & ~7) * 4 if p.split > 1 else 0)
+    tested = {(tile, split > 1) for _, _, _, tile, split in LOOPS}
+    assert picked <= tested, picked - tested
+    for tile, divided in tested:
+        if not divided:
+            assert {-(-K // 256) % 2 for _, K, _, t, s in LOOPS if t == tile and s == 1} == {0, 1}, tile
